@@ -431,6 +431,109 @@ int locret_adamw_step(float *param, void *param_bf16, const float *grad, float *
                       void *stream);
 
 /*
+ * ---- Several requests over one pool of pages ----
+ *
+ * A layer object holds the retained units of one request and decodes it alone.  The calls below decode a batch: the units of
+ * all requests lie in pages of one pool (one pool for each decoder layer, all with the same table), a table names each
+ * request's pages, and every step runs  locret_pages_step  once, then for each decoder layer  locret_norm_rope  (the new
+ * tokens' queries and keys, the latter with their values into the pages) and  locret_paged_attention.  A request that was
+ * prefilled and evicted in a layer object enters the pool by  locret_export_pages.  Unit i of a request (i-th in temporal
+ * order) sits at position i, as in a layer's cache (Section 3.4).
+ *
+ * None of these calls allocates, synchronises or keeps anything between calls: they may be captured into a graph, and calls on
+ * several streams may overlap as long as they do not write the same memory (a workspace counts).  What the host cannot see -
+ * values that lie on the device - is checked there: an entry outside its range is not followed, and *status (device int32,
+ * may be NULL; the caller sets it to 0 and reads it when it likes) becomes LOCRET_ERR_INVALID or LOCRET_ERR_CAPACITY, the
+ * lower of the codes where there are several.
+ */
+enum { LOCRET_BF16 = 0, LOCRET_FP16 = 1 };   /* dtype arguments */
+
+#define LOCRET_MAX_REQUESTS 4096             /* requests in one call */
+
+/* One layer's pool.  Column c of the key of token i of KV head m in page p: k + p * page_stride + m * head_stride +
+ * i * token_stride + c, in elements; values likewise.  Pointers 16-byte aligned, strides multiples of 8 and >= 0. */
+typedef struct {
+  void *k, *v;
+  int32_t n_pages, page_size, n_kv_heads, head_dim;   /* page_size: tokens per page, any number >= 1 */
+  int32_t dtype;
+  int64_t page_stride, head_stride, token_stride;
+} locret_pages;
+
+/*
+ * One step's bookkeeping, in one launch.  Request r holds lens_in[r] tokens in the pages table[r * table_stride + j],
+ * j < ceil(lens_in[r] / page_size) <= width.  new_lens[r] > 0: that many tokens join it, and the pages they need are taken from
+ * the end of the list free_pages[0 .. n_free), requests in order; 0: nothing; < 0: the request has ended, its pages go to the
+ * end of the list (before any is taken, so this step may use them) and its length becomes 0.  The new tokens are the rows of
+ * the step, requests in order: row t of request r, i-th of its new ones, has position lens_in[r] + i and slot
+ * page * page_size + offset.  Outputs (all device memory): lens_out [n_req] (may be lens_in), n_free_out (one word, may be
+ * n_free_in), the new entries of table and free_pages in place (nothing else in them changes), slots int64 [n_tok], positions
+ * [n_tok], starts [n_req + 1] (first row of every request; the last entry is the number of rows taken).  Rows behind the last
+ * new token: slot -1, position 0 (locret_norm_rope skips slot -1).  capacity: entries free_pages has room for, the number of
+ * pages of the pool.
+ * A request is refused - table, list and length as they were, its rows get slot -1 - if its length is outside
+ * [0, width * page_size] (LOCRET_ERR_INVALID), or if its tokens have no room in width pages, in n_tok rows or in what is left
+ * of the list after the requests before it, refused ones counted (LOCRET_ERR_CAPACITY).
+ * 0 <= n_req <= LOCRET_MAX_REQUESTS, 0 <= n_tok, 1 <= page_size, width, capacity.  The arrays must not overlap otherwise.
+ */
+int locret_pages_step(int32_t *table, int64_t table_stride, int32_t width, const int32_t *lens_in, int32_t *lens_out,
+                      const int32_t *new_lens, int32_t n_req, int32_t page_size, int32_t *free_pages, int32_t capacity,
+                      const int32_t *n_free_in, int32_t *n_free_out, int32_t n_tok, int64_t *slots, int32_t *positions,
+                      int32_t *starts, int32_t *status, void *stream);
+
+/*
+ * The retained units of a layer into pages: keys rotated at their positions and values, unit i of the layer (temporal order)
+ * into token i % page_size of page table_row[i / page_size] (device int32 [width]).  Asynchronous on the layer's stream, after
+ * whatever the layer has in flight.  The pool is bf16 with the layer's KV heads and head_dim; LOCRET_ERR_INVALID for a 4-bit
+ * cache and for a budget per KV head, LOCRET_ERR_CAPACITY if len > width * page_size.
+ */
+int locret_export_pages(locret_layer *layer, const locret_pages *pages, const int32_t *table_row, int32_t width,
+                        int32_t *status);
+
+/*
+ * Norms of queries and keys for each head, the rotation at the tokens' positions, and the cache append, in one pass:
+ *     n = x * g / sqrt(mean(x^2) + eps)   over the head's d elements, where g_q / g_k are given; else n = x
+ *     the first `rot` elements of n are rotated in pairs (i, i + rot/2), or (2i, 2i+1) if interleaved, pair i < rot/2 by
+ *     position * (2 pi turns[i] / 2^64), and multiplied by `factor`; the others stay.
+ * turns: device uint64 [rot/2], the pairs' angles per position as fractions of a turn, in units of 2^-64: whatever base and
+ * scaling for long contexts a model has is in them (and in factor), and position * turns modulo 2^64 is exact at every
+ * position.  Arithmetic in fp32, one rounding per element at the end.
+ * Element (t, j, c) of q: q + t * q_token + j * q_head + c, in elements, and so for k, v, q_out and k_out; pointers 16-byte
+ * aligned, strides multiples of 8.  q_out may be q and k_out k (same strides); otherwise outputs overlap nothing.
+ * pages (NULL: none): the rotated key and the value v of token t go to slot slots[t] (device int64; negative: skipped, beyond
+ * the pool: skipped and reported).  Slots must differ from each other.  k_out may be NULL if pages are given; v and slots are
+ * needed exactly if they are.
+ * 8 <= d <= 256, d a multiple of 8; rot a multiple of 8, 0 <= rot <= d; g_q, g_k of type dtype, 16-byte aligned, or NULL.
+ */
+typedef struct {
+  const void *q, *k, *v;
+  void *q_out, *k_out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+  int64_t q_out_token, q_out_head, k_out_token, k_out_head;
+  const int32_t *positions;        /* device [n_tok] */
+  const uint64_t *turns;
+  const void *g_q, *g_k;
+  const locret_pages *pages;       /* host struct */
+  const int64_t *slots;
+  int32_t *status;                 /* device, or NULL */
+  int32_t n_tok, n_q_heads, n_kv_heads, head_dim, rot, interleaved, dtype;
+  float factor, eps;
+} locret_rope_args;
+
+int locret_norm_rope(const locret_rope_args *args, void *stream);
+
+/*
+ * Its gradients.  args as in the forward call, but q_out and k_out hold dL/dq_out and dL/dk_out (read), and pages, slots and v
+ * are not looked at; q and k are the forward call's inputs (read only where there is a norm, may be NULL else).
+ * d_q [n_tok x h x d], d_k [n_tok x h_kv x d]: type dtype, contiguous, 16-byte aligned, written whole; they may be the
+ * buffers that held dL/dq_out and dL/dk_out if those are contiguous.  d_g_q, d_g_k: fp32 [d], given exactly where the norm is:
+ * sums over tokens and heads, in an order that depends on the sizes alone.  workspace: device memory, 16-byte aligned, at least
+ * the bytes that locret_norm_rope_grad_workspace reports (0 if there is no norm); contents need not be kept.
+ */
+int locret_norm_rope_grad_workspace(int32_t head_dim, int64_t *bytes);
+int locret_norm_rope_grad(const locret_rope_args *args, void *d_q, void *d_k, float *d_g_q, float *d_g_k, void *workspace,
+                          int64_t workspace_bytes, void *stream);
+
+/*
  * Retaining-head scores without any allocation.  (The paper has no counterpart: this entry
  * point exists for hosts that may not allocate device memory where they need scores, e.g. code
  * that runs inside a pool owning the whole device, or under an allocator that is locked while

@@ -22,3 +22,11 @@ from .binding import (  # noqa: F401
     rh_loss_grad,
     shard_by_kv_head,
 )
+from .paged import (  # noqa: F401
+    Pages,
+    PagesStep,
+    norm_rope,
+    norm_rope_grad,
+    pages_step,
+    rope_turns,
+)

@@ -40,6 +40,29 @@ class locret_block_cfg(C.Structure):
     ]
 
 
+class locret_pages(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("dtype", C.c_int32),
+        ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+    ]
+
+
+class locret_rope_args(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p), ("k_out", C.c_void_p),
+        ("q_token", C.c_int64), ("q_head", C.c_int64), ("k_token", C.c_int64), ("k_head", C.c_int64),
+        ("v_token", C.c_int64), ("v_head", C.c_int64),
+        ("q_out_token", C.c_int64), ("q_out_head", C.c_int64), ("k_out_token", C.c_int64), ("k_out_head", C.c_int64),
+        ("positions", C.c_void_p), ("turns", C.c_void_p), ("g_q", C.c_void_p), ("g_k", C.c_void_p),
+        ("pages", C.POINTER(locret_pages)), ("slots", C.c_void_p), ("status", C.c_void_p),
+        ("n_tok", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("rot", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32),
+        ("factor", C.c_float), ("eps", C.c_float),
+    ]
+
+
 def _load():
     if not os.path.exists(lib_path):
         raise ImportError(
@@ -89,6 +112,12 @@ def _load():
     l.locret_rh_loss_grad_ws.argtypes = [P, P, P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_float, P, P, P, P,
                                          C.c_int64, P]
     l.locret_adamw_step.argtypes = [P, P, P, P, P, C.c_int64, C.c_int32, C.c_float, C.c_float, C.c_float, C.c_float, C.c_float, P]
+    l.locret_pages_step.argtypes = [P, C.c_int64, C.c_int32, P, P, P, C.c_int32, C.c_int32, P, C.c_int32, P, P, C.c_int32, P,
+                                    P, P, P, P]
+    l.locret_export_pages.argtypes = [P, C.POINTER(locret_pages), P, C.c_int32, P]
+    l.locret_norm_rope.argtypes = [C.POINTER(locret_rope_args), P]
+    l.locret_norm_rope_grad_workspace.argtypes = [C.c_int32, C.POINTER(C.c_int64)]
+    l.locret_norm_rope_grad.argtypes = [C.POINTER(locret_rope_args), P, P, P, P, P, C.c_int64, P]
     l.locret_cis_labels.argtypes = [P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_float, P, P]
     return l
 
@@ -205,6 +234,13 @@ class LocretLayer:
         Ks, Vs = ks.astype(np.float32), vs.astype(np.float32)
         return dict(Kc=Kc, Vc=Vc, Ks=Ks, Vs=Vs, K=Kc * Ks[..., None], V=Vc * Vs[..., None],
                     S=S, T=T, seen=seen.value)
+
+    def export_pages(self, pages, table_row: torch.Tensor, status: torch.Tensor | None = None):
+        """The retained units into pages (a Pages): unit i into token i % page_size of page table_row[i // page_size]."""
+        if not (table_row.is_cuda and table_row.dtype == torch.int32 and table_row.dim() == 1 and table_row.is_contiguous()):
+            raise ValueError("table_row must be a contiguous CUDA int32 vector")
+        _check(lib.locret_export_pages(self._h, C.byref(pages.c), table_row.data_ptr(), table_row.numel(),
+                                       status.data_ptr() if status is not None else None), "locret_export_pages")
 
     def import_state_int4(self, Kc, Ks, Vc, Vs, S, T, seen: int):
         """Codes int8 [h_kv, len, d] in [-8, 7]; scales [h_kv, len] (values exact in fp16)."""

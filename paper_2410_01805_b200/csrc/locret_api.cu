@@ -11,6 +11,7 @@
 
 #include "../../include/locret.h"
 #include "common.cuh"
+#include "paged.cuh"
 #include "tc_common.cuh"
 
 using namespace locret;
@@ -1021,6 +1022,23 @@ int locret_export_state(locret_layer *L, void *K, void *V, float *scores, int64_
     if (scores && (rc = ord.copy_out(L, L->s, 4, scores)) != LOCRET_OK) return rc;
     if (token_ids && (rc = ord.copy_out(L, L->tid, 8, token_ids)) != LOCRET_OK) return rc;
   }
+  return LOCRET_OK;
+}
+
+int locret_export_pages(locret_layer *L, const locret_pages *pages, const int32_t *table_row, int32_t width, int32_t *status) {
+  if (!L || !on_layer_device(L) || !pages || !table_row || width < 1 || !pages_ok(*pages)) return LOCRET_ERR_INVALID;
+  if (pages->dtype != LOCRET_BF16 || pages->n_kv_heads != L->h_kv || pages->head_dim != L->d) return LOCRET_ERR_INVALID;
+  if (L->int4 || L->per_head || L->tp_pending) return LOCRET_ERR_INVALID;
+  if (L->len > (int64_t)width * pages->page_size) return LOCRET_ERR_CAPACITY;
+  if (L->len == 0) return LOCRET_OK;
+  // a selection / compaction in flight on the second stream still moves units
+  if (L->use_side && L->side_pending) {
+    CK(cudaStreamWaitEvent(L->st, L->ev_side, 0));
+    L->side_pending = false;
+  }
+  L->launches++;
+  CK(launch_export_pages(L->k_rot, L->v, L->rank[L->rcur], L->h_kv, L->d, L->cap, L->len,
+                         L->ranked_len < L->len ? L->ranked_len : L->len, table_row, *pages, status, L->st));
   return LOCRET_OK;
 }
 
