@@ -534,6 +534,28 @@ int locret_norm_rope_grad(const locret_rope_args *args, void *d_q, void *d_k, fl
                           int64_t workspace_bytes, void *stream);
 
 /*
+ * Decoding a batch (Eq. 1 with B = 1 for each request): row r of q is the newest token of request r, at position lens[r] - 1,
+ * whose key and value are already in the pages; it sees the request's keys j < lens[r], with window > 0 only those with
+ * j < sinks or j >= lens[r] - window (the newest `window` tokens, its own among them, and the first `sinks`):
+ *     out[r][j] = sum_i softmax_i(scale * q[r][j] . k_i) v_i ,   KV head j / (h / h_kv)
+ * A request of length 0 gets zeros.  Pages that hold no visible key are not read, and their table entries not looked at.
+ * Several requests may name the same pages.
+ * q, out: type of the pool, element (r, j, c) at r * *_req + j * *_head + c, 16-byte aligned, strides multiples of 8; lse: fp32
+ * [n_req x h] or NULL, the logarithm of the sum of exp(scale * q . k) (-inf for length 0).  table, lens: device int32 as in
+ * locret_pages_step; a length outside [0, width * page_size] is taken as the nearer end, a key in a page that does not exist
+ * as absent, both reported.  scale: any finite number (1 / sqrt(d) in Eq. 1).  head_dim 64, 96 or 128; h a multiple of h_kv;
+ * 0 <= n_req <= LOCRET_MAX_REQUESTS.
+ * Scores, softmax and sums in fp32; the probabilities enter the second product as the sum of two 16-bit numbers.
+ * workspace: device memory, 16-byte aligned, at least the bytes that locret_paged_attention_workspace reports for the current
+ * device; contents need not be kept, and two calls that may overlap need one each.
+ */
+int locret_paged_attention_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t *bytes);
+int locret_paged_attention(const void *q, int64_t q_req, int64_t q_head, const locret_pages *pages, const int32_t *table,
+                           int64_t table_stride, int32_t width, const int32_t *lens, int32_t n_req, int32_t n_q_heads,
+                           float scale, int32_t window, int32_t sinks, void *out, int64_t out_req, int64_t out_head, float *lse,
+                           int32_t *status, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Retaining-head scores without any allocation.  (The paper has no counterpart: this entry
  * point exists for hosts that may not allocate device memory where they need scores, e.g. code
  * that runs inside a pool owning the whole device, or under an allocator that is locked while

@@ -27,6 +27,7 @@ from .paged import (  # noqa: F401
     PagesStep,
     norm_rope,
     norm_rope_grad,
+    paged_attention,
     pages_step,
     rope_turns,
 )

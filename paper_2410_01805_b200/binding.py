@@ -118,6 +118,9 @@ def _load():
     l.locret_norm_rope.argtypes = [C.POINTER(locret_rope_args), P]
     l.locret_norm_rope_grad_workspace.argtypes = [C.c_int32, C.POINTER(C.c_int64)]
     l.locret_norm_rope_grad.argtypes = [C.POINTER(locret_rope_args), P, P, P, P, P, C.c_int64, P]
+    l.locret_paged_attention_workspace.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+    l.locret_paged_attention.argtypes = [P, C.c_int64, C.c_int64, C.POINTER(locret_pages), P, C.c_int64, C.c_int32, P, C.c_int32,
+                                         C.c_int32, C.c_float, C.c_int32, C.c_int32, P, C.c_int64, C.c_int64, P, P, P, C.c_int64, P]
     l.locret_cis_labels.argtypes = [P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_float, P, P]
     return l
 

@@ -1,0 +1,520 @@
+// Attention of one new token per request over pages, divided over the GPU and joined.
+//
+// Bound by memory: every visible key and value is read once, 4 d bytes of each for 4 g d operations.  So the kernel is a
+// stream of asynchronous copies with the arithmetic hidden behind it:
+//  * The visible keys of every (request, KV head) are cut into steps of 64, and all steps of the batch, one after the other,
+//    form a line that is cut into equal parts, one for each block of a persistent grid: lengths may differ as they like, and
+//    one long request fills the GPU as well as many short ones.  Every block finds its part by summing the lengths itself.
+//  * A warp takes 16 keys of each step and has a ring of stages of its own, filled by its own copies: no barrier of the block
+//    stands in the loop.  Keys are the m side of m16n8k16 tiles and the heads of a group (eight; sixteen in two tiles) the n
+//    side: S^T = K Q^T, O^T = V^T P^T, with an 8 x 8 transpose of P in between.
+//  * The softmax keeps a running scale per head that is raised only when a score exceeds it by 2^8 (then the 16 keys' maximum
+//    is found and the sums are rescaled): most steps need one vote in place of the reductions.
+//  * The warps of a block meet at the end of a (request, KV head); where the line was cut inside one, the blocks leave partial
+//    results that a second kernel joins, in the order of the blocks.
+#include <math.h>
+
+#include "../../include/locret.h"
+#include "common.cuh"
+#include "paged.cuh"
+
+namespace locret {
+namespace {
+
+constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32, PA_STEP = PA_WARPS * 16, PA_STAGES = 3, PA_PER_SM = 2;
+constexpr float PA_RAISE = 8.0f;   // log2 of how far a score may exceed the running scale
+
+template <typename T>
+__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16<bf16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+
+struct PagedAttn {
+  const void *q;
+  void *out;
+  float *lse, *part;       // part: [block][2] partial results of HB heads: sums [HB][d], then (scale, sum) [HB][2]
+  int4 *rec;               // [block]: x = request whose part begins in the block and does not end there (-1: none), y = its
+                           // item, z = 1 if the block's first part goes on behind it, 2 if it ends there (0: none)
+  const int32_t *table, *lens;
+  int32_t *status;
+  PageView pages;
+  long long q_req, q_head, out_req, out_head, table_stride;
+  int width, n_req, h, h_kv, groups, window, sinks;   // groups: blocks of heads per KV head
+  float scale_log2;
+};
+
+// A request's visible keys, numbered 0 .. n-1: key i is i for i < sinks, else i + shift.
+struct Visible {
+  int n, shift, sinks;
+  __device__ __forceinline__ int key(int i) const { return i < sinks ? i : i + shift; }
+  __device__ __forceinline__ int steps() const { return n > 0 ? (n - 1) / PA_STEP + 1 : 1; }   // (an empty request has one, to write zeros)
+};
+__device__ __forceinline__ int clamped_len(const PagedAttn &a, int r) {
+  const int n = __ldg(a.lens + r);
+  return max(0, (int)min((long long)n, (long long)a.width * a.pages.page_size));
+}
+__device__ __forceinline__ Visible visible_of(const PagedAttn &a, int len) {
+  Visible v = {len, 0, 0};
+  if (a.window > 0) {
+    const int start = max(a.sinks, len - a.window);
+    v.sinks = a.sinks;
+    v.shift = start - a.sinks;
+    v.n = min(len, a.sinks) + max(0, len - start);
+  }
+  return v;
+}
+
+// A place in the line: step `tile` of item `item` (KV head, block of heads) of request r.
+struct Cursor {
+  int r, item, tile, steps;
+  Visible v;
+  __device__ __forceinline__ void enter(const PagedAttn &a, int request) {
+    r = request;
+    v = visible_of(a, clamped_len(a, min(r, a.n_req - 1)));
+    steps = v.steps();
+  }
+  __device__ __forceinline__ void next(const PagedAttn &a, int items) {
+    if (++tile < steps) return;
+    tile = 0;
+    if (++item < items) return;
+    item = 0;
+    enter(a, r + 1);
+  }
+};
+
+// The block's part [lo, hi) of the line, the request in which it begins, and how far into the request (in steps of all its
+// items).  With fewer steps than blocks the first blocks take one each, so that no block between two parts of an item is empty.
+__device__ void find(const PagedAttn &a, int items, long long &lo, long long &hi, int &r_out, long long &into) {
+  __shared__ long long warp_sums[PA_WARPS], found_into;
+  __shared__ int found_r;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (a.n_req + PA_THREADS - 1) / PA_THREADS, r0 = min(a.n_req, tid * per), r1 = min(a.n_req, r0 + per);
+  long long mine = 0;
+  for (int r = r0; r < r1; r++) {
+    const int raw = __ldg(a.lens + r), len = clamped_len(a, r);
+    if (raw != len && blockIdx.x == 0) report(a.status, LOCRET_ERR_INVALID);
+    mine += visible_of(a, len).steps();
+  }
+  long long x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  long long before = x - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < PA_WARPS; w++) {
+    if (w < warp) before += warp_sums[w];
+    total += warp_sums[w];
+  }
+  total *= items;
+  const long long parts = min((long long)gridDim.x, total), part = min((long long)blockIdx.x, parts);
+  lo = total * part / parts;
+  hi = part < parts ? total * (part + 1) / parts : lo;
+  if (lo < hi && before * items <= lo && lo < (before + mine) * items) {
+    long long rest = lo - before * items;
+    int r = r0;
+    for (; r < r1; r++) {
+      const long long n = (long long)visible_of(a, clamped_len(a, r)).steps() * items;
+      if (rest < n) break;
+      rest -= n;
+    }
+    found_r = r;
+    found_into = rest;
+  }
+  __syncthreads();
+  r_out = found_r;
+  into = found_into;
+}
+
+template <typename T, int D, int NT>
+struct PaSmem {
+  static constexpr int LD = D + 8, HB = 8 * NT, LF = D / 2 + 4;   // (rows of both spread over the banks)
+  static constexpr int STAGE = 2 * 16 * LD * 2;                   // bytes: keys and values of a warp's 16
+  static constexpr int BYTES = PA_WARPS * PA_STAGES * STAGE + PA_WARPS * 8 * LF * 4;
+};
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const __grid_constant__ PagedAttn a) {
+  using S = PaSmem<T, D, NT>;
+  constexpr int LD = S::LD, HB = S::HB, LF = S::LF, VPR = D / 8, KD = D / 16;
+  extern __shared__ __align__(16) unsigned char pa_smem[];
+  __shared__ uint32_t there[PA_WARPS][PA_STAGES];                 // which of a stage's 16 keys exist
+  __shared__ float wm[PA_WARPS][HB], wl[PA_WARPS][HB];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g4 = lane >> 2, q4 = lane & 3;
+  const int g = a.h / a.h_kv, items = a.h_kv * a.groups;
+  T *const ring = reinterpret_cast<T *>(pa_smem + warp * PA_STAGES * S::STAGE);
+  float *const fo = reinterpret_cast<float *>(pa_smem + PA_WARPS * PA_STAGES * S::STAGE);   // [warp][8][LF]
+  pdl_launch_dependents();
+
+  long long lo, hi, into;
+  int r_first;
+  find(a, items, lo, hi, r_first, into);
+  int4 rec = make_int4(-1, 0, 0, 0);
+  if (lo >= hi) {
+    if (tid == 0) a.rec[blockIdx.x] = rec;
+    return;
+  }
+  const long long n_steps = hi - lo;
+
+  Cursor use;
+  use.enter(a, r_first);
+  use.item = (int)(into / use.steps);
+  use.tile = (int)(into - (long long)use.item * use.steps);
+  Cursor load = use;
+
+  // where the rows of the next step to be requested lie: lane (and lane + 16) = row of the warp's 16
+  long long row_at = 0;
+  bool row_there = false;
+  auto look_up = [&]() {
+    const int i = load.tile * PA_STEP + warp * 16 + (lane & 15);
+    row_there = i < load.v.n;
+    const int key = row_there ? load.v.key(i) : 0, j = key / a.pages.page_size;
+    const int page = row_there ? __ldg(a.table + load.r * a.table_stride + j) : 0;
+    if (page < 0 || page >= a.pages.n_pages) {
+      row_there = false;
+      report(a.status, LOCRET_ERR_INVALID);
+    }
+    const int m = load.item / a.groups;
+    row_at = row_there ? page * a.pages.page_stride + m * a.pages.head_stride + (key - j * a.pages.page_size) * a.pages.token_stride : 0;
+  };
+  auto request = [&](int stage) {
+    T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
+    const uint32_t mask = __ballot_sync(0xffffffffu, row_there) & 0xffffu;
+    if (lane == 0) there[warp][stage] = mask;
+#pragma unroll
+    for (int x = 0; x < 16 * VPR / 32; x++) {
+      const int c = x * 32 + lane, row = c / VPR, col = (c - row * VPR) * 8;
+      const long long at = __shfl_sync(0xffffffffu, row_at, row) + col;
+      const bool ok = (mask >> row) & 1;
+      cp_async16(ks + row * LD + col, static_cast<const T *>(a.pages.k) + at, ok);
+      cp_async16(vs + row * LD + col, static_cast<const T *>(a.pages.v) + at, ok);
+    }
+  };
+  long long asked = 0;
+  look_up();
+#pragma unroll
+  for (int s = 0; s < PA_STAGES - 1; s++) {
+    if (asked < n_steps) {
+      request(s);
+      load.next(a, items);
+      if (++asked < n_steps) look_up();
+    }
+    cp_async_commit();
+  }
+
+  uint32_t qf[NT][KD][2];
+  float o[NT][KD][4], m_run[NT][2], l_run[NT][2];
+  bool fresh = true;      // the state below belongs to no item yet
+  int first_tile = 0, stage = 0;
+  for (long long step = 0; step < n_steps; step++) {
+    if (fresh) {
+      fresh = false;
+      first_tile = use.tile;
+      const int m = use.item / a.groups, hg = use.item - m * a.groups;
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++) {
+        const int head = hg * HB + nt * 8 + g4;   // within the group
+        const T *row = static_cast<const T *>(a.q) + use.r * a.q_req + (m * g + min(head, g - 1)) * a.q_head + q4 * 2;
+#pragma unroll
+        for (int kk = 0; kk < KD; kk++) {
+          qf[nt][kk][0] = head < g ? *reinterpret_cast<const uint32_t *>(row + kk * 16) : 0u;
+          qf[nt][kk][1] = head < g ? *reinterpret_cast<const uint32_t *>(row + kk * 16 + 8) : 0u;
+        }
+#pragma unroll
+        for (int kk = 0; kk < KD; kk++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) o[nt][kk][e] = 0.f;
+        m_run[nt][0] = m_run[nt][1] = -INFINITY;
+        l_run[nt][0] = l_run[nt][1] = 0.f;
+      }
+    }
+    cp_async_wait<PA_STAGES - 2>();
+    __syncwarp();   // the other lanes' copies too; and all lanes are done with the stage that is refilled now
+    if (asked < n_steps) {
+      request(stage == 0 ? PA_STAGES - 1 : stage - 1);   // (the stage of the last step)
+      load.next(a, items);
+      if (++asked < n_steps) look_up();
+    }
+    cp_async_commit();
+
+    const T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
+    const uint32_t mask = there[warp][stage];
+    if (mask) {
+      float s[NT][4] = {};
+#pragma unroll
+      for (int kk = 0; kk < KD; kk++) {
+        uint32_t a0, a1, a2, a3;
+        ldmatrix_x4(a0, a1, a2, a3, ks + (lane & 15) * LD + kk * 16 + (lane >> 4) * 8);
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) mma16<T>(s[nt], a0, a1, a2, a3, qf[nt][kk][0], qf[nt][kk][1]);
+      }
+      // s[nt]: keys g4, g4, g4 + 8, g4 + 8 of heads 2 q4, 2 q4 + 1, 2 q4, 2 q4 + 1
+      bool raise = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          s[nt][e] = (mask >> (g4 + (e >> 1) * 8)) & 1 ? s[nt][e] * a.scale_log2 : -INFINITY;
+          raise |= s[nt][e] > m_run[nt][e & 1] + PA_RAISE;
+        }
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+          float alpha[2];
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            float t = fmaxf(s[nt][e], s[nt][e + 2]);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
+            const float top = fmaxf(m_run[nt][e], t);
+            alpha[e] = exp2f(m_run[nt][e] - (top == -INFINITY ? 0.f : top));
+            m_run[nt][e] = top;
+            l_run[nt][e] *= alpha[e];
+          }
+#pragma unroll
+          for (int kk = 0; kk < KD; kk++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) o[nt][kk][e] *= alpha[e & 1];
+        }
+      }
+      // P^T, as the sum of two 16-bit numbers: the high part and what it leaves
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+          float p[2];
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            const float m = m_run[nt][e];
+            p[e] = exp2f(s[nt][half * 2 + e] - (m == -INFINITY ? 0.f : m));
+            l_run[nt][e] += p[e];
+          }
+          const uint32_t hi16 = Half2<T>::pack(p[0], p[1]);
+          const float2 back = Half2<T>::unpack(hi16);
+          ph[nt][half] = transpose8x8(hi16);
+          pl[nt][half] = transpose8x8(Half2<T>::pack(p[0] - back.x, p[1] - back.y));
+        }
+#pragma unroll
+      for (int kk = 0; kk < KD; kk++) {
+        uint32_t a0, a1, a2, a3;
+        ldmatrix_x4_trans(a0, a1, a2, a3, vs + ((lane & 7) + (lane >> 4) * 8) * LD + kk * 16 + ((lane >> 3) & 1) * 8);
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+          mma16<T>(o[nt][kk], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+          mma16<T>(o[nt][kk], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+        }
+      }
+    }
+    __syncwarp();
+
+    const bool ends = use.tile + 1 == use.steps;
+    if (ends || step + 1 == n_steps) {
+      // ---- the warps meet
+      const bool whole = ends && first_tile == 0, begins = first_tile == 0;
+      const int m = use.item / a.groups, hg = use.item - m * a.groups, gh = min(HB, g - hg * HB);
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) l_run[nt][e] += __shfl_xor_sync(0xffffffffu, l_run[nt][e], x);
+          if (g4 == 0) { wm[warp][nt * 8 + q4 * 2 + e] = m_run[nt][e]; wl[warp][nt * 8 + q4 * 2 + e] = l_run[nt][e]; }
+        }
+      __syncthreads();
+      float *const part = a.part + ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * (HB * (D + 2));
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++) {
+        float w[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const int c = nt * 8 + q4 * 2 + e;
+          const float top = fmaxf(fmaxf(wm[0][c], wm[1][c]), fmaxf(wm[2][c], wm[3][c]));
+          w[e] = exp2f(m_run[nt][e] - (top == -INFINITY ? 0.f : top));
+        }
+#pragma unroll
+        for (int side = 0; side < 2; side++) {
+#pragma unroll
+          for (int kk = 0; kk < KD / 2; kk++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+              fo[(warp * 8 + q4 * 2 + (e & 1)) * LF + kk * 16 + g4 + (e >> 1) * 8] = o[nt][side * (KD / 2) + kk][e] * w[e & 1];
+          __syncthreads();
+          for (int x = tid; x < 8 * (D / 8); x += PA_THREADS) {   // (head, four columns of this half)
+            const int hh = x / (D / 8), c = (x - hh * (D / 8)) * 4, head = nt * 8 + hh, col = side * (D / 2) + c;
+            if (head >= gh) continue;
+            float top = wm[0][head], l = 0.f;
+#pragma unroll
+            for (int v = 1; v < PA_WARPS; v++) top = fmaxf(top, wm[v][head]);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int v = 0; v < PA_WARPS; v++) {
+              const float4 f = *reinterpret_cast<const float4 *>(fo + (v * 8 + hh) * LF + c);
+              sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
+              l += wl[v][head] * exp2f(wm[v][head] - ref);
+            }
+            const int j = m * g + hg * HB + head;
+            if (whole) {
+              const float inv = use.v.n > 0 ? 1.0f / l : 0.f;
+              *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + use.r * a.out_req + j * a.out_head + col) =
+                  make_uint2(Half2<T>::pack(sum.x * inv, sum.y * inv), Half2<T>::pack(sum.z * inv, sum.w * inv));
+              if (a.lse && col == 0) a.lse[(size_t)use.r * a.h + j] = use.v.n > 0 ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            } else {
+              *reinterpret_cast<float4 *>(part + head * D + col) = sum;
+              if (col == 0) *reinterpret_cast<float2 *>(part + HB * D + head * 2) = make_float2(top, l);
+            }
+          }
+          __syncthreads();
+        }
+      }
+      if (!whole) {
+        if (begins) { rec.x = use.r; rec.y = use.item; }
+        else rec.z = ends ? 2 : 1;
+      }
+      fresh = true;
+    }
+    use.next(a, items);
+    stage = stage + 1 == PA_STAGES ? 0 : stage + 1;
+  }
+  cp_async_wait<0>();
+  if (tid == 0) a.rec[blockIdx.x] = rec;
+}
+
+// Block b joins the item that begins in block b's part of the line and ends in another's: one warp a head, lanes over columns.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ PagedAttn a) {
+  constexpr int HB = 8 * NT, C = D / 32;
+  pdl_wait();
+  const int b = blockIdx.x, lane = threadIdx.x & 31, head = blockIdx.y * 4 + (threadIdx.x >> 5);
+  const int4 rec = a.rec[b];
+  if (rec.x < 0) return;
+  const int g = a.h / a.h_kv, m = rec.y / a.groups, hg = rec.y - m * a.groups;
+  if (head >= min(HB, g - hg * HB)) return;
+  // its parts: the second of block b, the first of the blocks behind it up to the one where it ends
+  int n = 1;
+  for (int at = b + 1;; at += 32) {
+    const bool end = at + lane < gridDim.x ? a.rec[at + lane].z == 2 : true;
+    const unsigned ends = __ballot_sync(0xffffffffu, end);
+    if (ends) { n += at - b - 1 + __ffs(ends); break; }
+  }
+  auto part = [&](int i) { return a.part + ((size_t)(b + i) * 2 + (i == 0 ? 1 : 0)) * (HB * (D + 2)); };
+  float top = -INFINITY;
+  for (int i = lane; i < n; i += 32) top = fmaxf(top, part(i)[HB * D + head * 2]);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float l = 0.f, acc[C] = {};
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    float w = 0.f;
+    if (i0 + lane < n) {
+      const float2 ml = *reinterpret_cast<const float2 *>(part(i0 + lane) + HB * D + head * 2);
+      w = exp2f(ml.x - ref);
+      l += w * ml.y;
+    }
+    const int count = min(32, n - i0);
+#pragma unroll 8
+    for (int i = 0; i < count; i++) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      const float *o = part(i0 + i) + head * D + lane;
+#pragma unroll
+      for (int c = 0; c < C; c++) acc[c] = fmaf(wi, o[c * 32], acc[c]);
+    }
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+  const int j = m * g + hg * HB + head;
+  T *out = static_cast<T *>(a.out) + rec.x * a.out_req + j * a.out_head + lane;
+#pragma unroll
+  for (int c = 0; c < C; c++) {
+    const uint32_t v = Half2<T>::pack(acc[c] / l, 0.f);
+    *reinterpret_cast<uint16_t *>(out + c * 32) = (uint16_t)v;
+  }
+  if (a.lse && lane == 0) a.lse[(size_t)rec.x * a.h + j] = (top + log2f(l)) * 0.6931471805599453f;
+}
+
+int heads_per_block(int h, int h_kv) { return h / h_kv > 8 ? 16 : 8; }
+int paged_blocks() { return sm_count_of_current_device() * PA_PER_SM; }
+size_t part_floats(int h, int h_kv, int d) { return (size_t)heads_per_block(h, h_kv) * (d + 2); }
+
+template <typename T, int D, int NT>
+cudaError_t launch(const PagedAttn &a, cudaStream_t st) {
+  using S = PaSmem<T, D, NT>;
+  static PerDeviceFlag flag;
+  cudaError_t e = allow_dynamic_smem(paged_attn_kernel<T, D, NT>, S::BYTES, flag);
+  if (e != cudaSuccess) return e;
+  const int blocks = paged_blocks();
+  e = launch_kernel(paged_attn_kernel<T, D, NT>, dim3(blocks), dim3(PA_THREADS), S::BYTES, st, false, a);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(paged_join_kernel<T, D, NT>, dim3(blocks, NT * 2), dim3(128), 0, st, true, a);
+}
+
+template <typename T>
+cudaError_t launch_by_size(const PagedAttn &a, int d, int nt, cudaStream_t st) {
+  if (nt == 1) return d == 64 ? launch<T, 64, 1>(a, st) : d == 96 ? launch<T, 96, 1>(a, st) : launch<T, 128, 1>(a, st);
+  return d == 64 ? launch<T, 64, 2>(a, st) : d == 96 ? launch<T, 96, 2>(a, st) : launch<T, 128, 2>(a, st);
+}
+
+bool heads_ok(int32_t h, int32_t h_kv, int32_t d) {
+  return h >= 1 && h_kv >= 1 && h <= 65536 && h % h_kv == 0 && (d == 64 || d == 96 || d == 128);
+}
+bool aligned16p(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace
+}  // namespace locret
+
+using namespace locret;
+
+extern "C" int locret_paged_attention_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t *bytes) {
+  if (!bytes || !heads_ok(n_q_heads, n_kv_heads, head_dim)) return LOCRET_ERR_INVALID;
+  *bytes = (int64_t)paged_blocks() * (sizeof(int4) + 2 * sizeof(float) * part_floats(n_q_heads, n_kv_heads, head_dim));
+  return LOCRET_OK;
+}
+
+extern "C" int locret_paged_attention(const void *q, int64_t q_req, int64_t q_head, const locret_pages *pages,
+                                      const int32_t *table, int64_t table_stride, int32_t width, const int32_t *lens,
+                                      int32_t n_req, int32_t n_q_heads, float scale, int32_t window, int32_t sinks, void *out,
+                                      int64_t out_req, int64_t out_head, float *lse, int32_t *status, void *workspace,
+                                      int64_t workspace_bytes, void *stream) {
+  if (!pages || !pages_ok(*pages) || !heads_ok(n_q_heads, pages->n_kv_heads, pages->head_dim)) return LOCRET_ERR_INVALID;
+  if (n_req < 0 || n_req > LOCRET_MAX_REQUESTS || width < 1 || table_stride < 0 || (n_req > 1 && table_stride < width) ||
+      window < 0 || sinks < 0 || !isfinite(scale))
+    return LOCRET_ERR_INVALID;
+  if ((q_req | q_head | out_req | out_head) & 7 || !aligned16p(q) || !aligned16p(out) || !aligned16p(workspace)) return LOCRET_ERR_INVALID;
+  if (n_req == 0) return LOCRET_OK;
+  if (!q || !table || !lens || !out || !workspace) return LOCRET_ERR_INVALID;
+  int64_t need = 0;
+  locret_paged_attention_workspace(n_q_heads, pages->n_kv_heads, pages->head_dim, &need);
+  if (workspace_bytes < need) return LOCRET_ERR_CAPACITY;
+  const int hb = heads_per_block(n_q_heads, pages->n_kv_heads), g = n_q_heads / pages->n_kv_heads;
+  PagedAttn a = {};
+  a.q = q; a.out = out; a.lse = lse; a.status = status;
+  a.rec = static_cast<int4 *>(workspace);
+  a.part = reinterpret_cast<float *>(a.rec + paged_blocks());
+  a.table = table; a.lens = lens; a.table_stride = table_stride;
+  a.pages = page_view(*pages);
+  a.q_req = q_req; a.q_head = q_head; a.out_req = out_req; a.out_head = out_head;
+  a.width = width; a.n_req = n_req; a.h = n_q_heads; a.h_kv = pages->n_kv_heads; a.groups = (g + hb - 1) / hb;
+  a.window = window; a.sinks = sinks;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const cudaError_t e = pages->dtype == LOCRET_BF16 ? launch_by_size<bf16>(a, pages->head_dim, hb / 8, (cudaStream_t)stream)
+                                                    : launch_by_size<__half>(a, pages->head_dim, hb / 8, (cudaStream_t)stream);
+  if (e != cudaSuccess) { cudaGetLastError(); return LOCRET_ERR_CUDA; }
+  return LOCRET_OK;
+}

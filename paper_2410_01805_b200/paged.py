@@ -1,4 +1,5 @@
-"""Several requests over one pool of pages: bookkeeping, norms / rotation / append, and their gradients (include/locret.h)."""
+"""Several requests over one pool of pages: bookkeeping, norms / rotation / append and their gradients, and
+attention of one new token each (include/locret.h)."""
 
 from __future__ import annotations
 
@@ -224,3 +225,30 @@ def norm_rope_grad(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor |
                                      dg_k.data_ptr() if dg_k is not None else None,
                                      ws.data_ptr() if ws is not None else None, need.value, stream), "locret_norm_rope_grad")
     return dq, dk, dg_q, dg_k
+
+
+def paged_attention(q: torch.Tensor, pages: Pages, table: torch.Tensor, lens: torch.Tensor, scale: float | None = None,
+                    window: int = 0, sinks: int = 0, out: torch.Tensor | None = None, with_lse: bool = False,
+                    status: torch.Tensor | None = None):
+    """Attention of each request's newest token, q [n_req, h, d], over the keys and values in its pages: table int32
+    [n_req, width], lens int32 [n_req] (the new token counted).  window > 0: only the last `window` and the first `sinks`
+    tokens are visible.  scale: 1 / sqrt(d) by default.  Returns out, [n_req, h, d], or (out, lse fp32 [n_req, h])."""
+    stream = _on_current_device(q, "q")
+    if q.dim() != 3 or pages.k.device != q.device or q.dtype != pages.k.dtype or q.shape[2] != pages.c.head_dim:
+        raise ValueError("q must be [n_req, h, d] of the pages' type, head size and device")
+    n, h, d = q.shape
+    if table.shape[:1] != (n,) or lens.shape != (n,):
+        raise ValueError("one row of the table and one length for every request")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty((n, h), dtype=torch.float32, device=q.device) if with_lse else None
+    need = C.c_int64()
+    _check(lib.locret_paged_attention_workspace(h, pages.c.n_kv_heads, d, C.byref(need)), "locret_paged_attention")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    _check(lib.locret_paged_attention(q.data_ptr(), *_heads(q, "q", q), C.byref(pages.c),
+                                      _words(table, torch.int32, 2, "table", q), table.stride(0), table.shape[1],
+                                      _words(lens, torch.int32, 1, "lens", q), n, h, d ** -0.5 if scale is None else scale,
+                                      window, sinks, out.data_ptr(), *_heads(out, "out", q, q.shape),
+                                      lse.data_ptr() if with_lse else None, _status(status, q), ws.data_ptr(), need.value,
+                                      stream), "locret_paged_attention")
+    return (out, lse) if with_lse else out
