@@ -114,7 +114,7 @@ def _load():
     l.locret_adamw_step.argtypes = [P, P, P, P, P, C.c_int64, C.c_int32, C.c_float, C.c_float, C.c_float, C.c_float, C.c_float, P]
     l.locret_pages_step.argtypes = [P, C.c_int64, C.c_int32, P, P, P, C.c_int32, C.c_int32, P, C.c_int32, P, P, C.c_int32, P,
                                     P, P, P, P]
-    l.locret_export_pages.argtypes = [P, C.POINTER(locret_pages), P, C.c_int32, P]
+    l.locret_export_pages.argtypes = [P, P, P, C.c_int32, P]
     l.locret_norm_rope.argtypes = [C.POINTER(locret_rope_args), P]
     l.locret_norm_rope_grad_workspace.argtypes = [C.c_int32, C.POINTER(C.c_int64)]
     l.locret_norm_rope_grad.argtypes = [C.POINTER(locret_rope_args), P, P, P, P, P, C.c_int64, P]
@@ -242,7 +242,7 @@ class LocretLayer:
         """The retained units into pages (a Pages): unit i into token i % page_size of page table_row[i // page_size]."""
         if not (table_row.is_cuda and table_row.dtype == torch.int32 and table_row.dim() == 1 and table_row.is_contiguous()):
             raise ValueError("table_row must be a contiguous CUDA int32 vector")
-        _check(lib.locret_export_pages(self._h, C.byref(pages.c), table_row.data_ptr(), table_row.numel(),
+        _check(lib.locret_export_pages(self._h, pages.address, table_row.data_ptr(), table_row.numel(),
                                        status.data_ptr() if status is not None else None), "locret_export_pages")
 
     def import_state_int4(self, Kc, Ks, Vc, Vs, S, T, seen: int):

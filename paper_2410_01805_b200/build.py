@@ -1,15 +1,21 @@
-"""Build the CUDA library (sm_100a only) in-tree: paper_2410_01805_b200/liblocret.so."""
+"""Build the CUDA library (sm_100a only) in-tree, paper_2410_01805_b200/liblocret.so, and the Python module that calls it
+without ctypes, _paged.so."""
 
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblocret.so")
+MODULE = os.path.join(HERE, "_paged.so")
+MODULE_SRC = os.path.join(CSRC, "paged_module.cpp")
+HEADER = os.path.join(HERE, "..", "include", "locret.h")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -30,9 +36,30 @@ def needs_build() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def module_needs_build() -> bool:
+    return not os.path.exists(MODULE) or any(os.path.getmtime(p) > os.path.getmtime(MODULE) for p in (MODULE_SRC, HEADER))
+
+
+def module_command():
+    """g++ against torch's headers and libraries (found without importing it); the library is looked for beside the module."""
+    torch = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *("-I" + p for p in include), MODULE_SRC,
+            "-o", MODULE, "-L" + HERE, "-l:liblocret.so", "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch",
+            "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
+    if force or needs_build():
+        build_library(force, verbose)
+    if force or module_needs_build():
+        subprocess.check_call(module_command())
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> None:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     objs = []
     os.makedirs(os.path.join(HERE, "build"), exist_ok=True)
@@ -59,7 +86,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
         raise RuntimeError("nvcc failed")
     subprocess.check_call([nvcc, "-shared", "-Wno-deprecated-gpu-targets", "-o", LIB, *objs,
                            "-lcudart_static", "-ldl", "-lrt", "-lpthread"])
-    return LIB
 
 
 if __name__ == "__main__":

@@ -359,6 +359,7 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
   const Item<E> it = Item<E>::template of<I>(j, p.d, p.rot);
   const Raw<E> gain_raw = load_item(g, it, g != nullptr);
   P2<E> dg = {};
+  pdl_launch_dependents();
   const int steps = (rows + R - 1) / R;
   const long long units = (long long)p.n_tok * part.slices, stride = (long long)part.blocks * NRG_WARPS;
   Ring<E, 2, NRG_STAGES> &ring = rings[warp];
@@ -464,10 +465,11 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
   }
 }
 
-// d_g = the blocks' partial sums: 32 columns a block, eight rows of threads over the partials
-__global__ void __launch_bounds__(256)
+// d_g = the blocks' partial sums: 32 columns a block, 32 rows of threads over the partials (a chain of latencies: eight rows
+// took 6 us longer for 444 partials)
+__global__ void __launch_bounds__(1024)
 norm_rope_gains_kernel(const float *__restrict__ partial, int q_blocks, int k_blocks, int d, float *d_g_q, float *d_g_k) {
-  __shared__ float sums[8][33];
+  __shared__ float sums[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x, w = blockIdx.y;
   float *out = w ? d_g_k : d_g_q;
   pdl_wait();
@@ -476,17 +478,15 @@ norm_rope_gains_kernel(const float *__restrict__ partial, int q_blocks, int k_bl
   const int n = w ? k_blocks : q_blocks;
   float s = 0.f;
   if (c < d) {
-#pragma unroll 8
-    for (int b = y; b < n; b += 8) s += from[(size_t)b * d + c];
+#pragma unroll 16
+    for (int b = y; b < n; b += 32) s += from[(size_t)b * d + c];
   }
   sums[y][x] = s;
   __syncthreads();
-  if (y == 0 && c < d) {
-    s = 0.f;
+  s = sums[x][y];   // warp y: column y, a lane for every row of threads
 #pragma unroll
-    for (int r = 0; r < 8; r++) s += sums[r][x];
-    out[c] = s;
-  }
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (x == 0 && blockIdx.x * 32 + y < d) out[blockIdx.x * 32 + y] = s;
 }
 
 bool aligned16p(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -559,7 +559,7 @@ cudaError_t launch_backward(const NormRope &p, void *d_q, void *d_k, float *d_g_
     if (e != cudaSuccess) return e;
   }
   if (!partial) return cudaSuccess;
-  return launch_kernel(norm_rope_gains_kernel, dim3((p.d + 31) / 32, 2), dim3(256), 0, st, true, (const float *)partial, q.blocks,
+  return launch_kernel(norm_rope_gains_kernel, dim3((p.d + 31) / 32, 2), dim3(1024), 0, st, true, (const float *)partial, q.blocks,
                        k.blocks, p.d, d_g_q, d_g_k);
 }
 
