@@ -275,7 +275,7 @@ norm_rope_kernel(const __grid_constant__ NormRope p, int slices) {
   if (p.pages.k) {
     const int64_t slot = p.slots[tok];
     if (slot >= 0) {
-      const int64_t page = slot <= INT32_MAX ? (int64_t)((uint32_t)slot / (uint32_t)p.pages.page_size) : slot / p.pages.page_size;
+      const int64_t page = slot <= INT32_MAX ? (int64_t)p.pages.by_size.div((int)slot) : slot / p.pages.page_size;
       if (page < p.pages.n_pages) place = page * p.pages.page_stride + (slot - page * p.pages.page_size) * p.pages.token_stride;
       else if (lane == 0) report(p.status, LOCRET_ERR_INVALID);
     }

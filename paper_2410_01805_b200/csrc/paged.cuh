@@ -6,14 +6,29 @@
 
 namespace locret {
 
+// n / d for 0 <= n < 2^31: n * ceil(2^(31 + s) / d) >> (31 + s) with s = ceil(log2 d), exact because the factor is too large by
+// less than 2^s / d * 2^-(31 + s) of itself.
+struct FastDiv {
+  uint32_t mul, shift;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) s++;
+    shift = 31 + s;
+    mul = (uint32_t)(((1ull << shift) + d - 1) / d);
+  }
+  __device__ __forceinline__ int div(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+};
+
 struct PageView {
   void *k, *v;
   long long page_stride, head_stride, token_stride;   // elements
   int n_pages, page_size;
+  FastDiv by_size;
 };
 
 inline PageView page_view(const locret_pages &p) {
-  return PageView{p.k, p.v, p.page_stride, p.head_stride, p.token_stride, p.n_pages, p.page_size};
+  return PageView{p.k, p.v, p.page_stride, p.head_stride, p.token_stride, p.n_pages, p.page_size, FastDiv(p.page_size)};
 }
 
 inline bool pages_ok(const locret_pages &p) {

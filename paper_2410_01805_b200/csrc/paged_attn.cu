@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
   auto look_up = [&]() {
     const int i = load.tile * PA_STEP + warp * 16 + (lane & 15);
     row_there = i < load.v.n;
-    const int key = row_there ? load.v.key(i) : 0, j = key / a.pages.page_size;
+    const int key = row_there ? load.v.key(i) : 0, j = a.pages.by_size.div(key);
     const int page = row_there ? __ldg(a.table + load.r * a.table_stride + j) : 0;
     if (page < 0 || page >= a.pages.n_pages) {
       row_there = false;
@@ -397,56 +397,94 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
   if (tid == 0) a.rec[blockIdx.x] = rec;
 }
 
-// Block b joins the item that begins in block b's part of the line and ends in another's: one warp a head, lanes over columns.
+// Block (b, head) joins that head of the item that begins in block b's part of the line and ends in another's.  A chain of
+// latencies (records, then parts): a thread takes four columns of every JOIN_AT_ONCE-th part and requests JOIN_BATCH of them
+// before it uses one (one 6000-token request, 38 parts an item: 22.9 us with a warp per head and a part after the other).
+constexpr int JOIN_THREADS = 128, JOIN_BATCH = 8;
+
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ PagedAttn a) {
-  constexpr int HB = 8 * NT, C = D / 32;
+__global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const __grid_constant__ PagedAttn a) {
+  constexpr int HB = 8 * NT, TPP = D / 4, AT_ONCE = JOIN_THREADS / TPP, PART = HB * (D + 2);
+  __shared__ float4 sums[AT_ONCE][TPP];
+  __shared__ float ls[AT_ONCE], tops[JOIN_THREADS / 32];
+  const int b = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = a.h / a.h_kv;
+  if (head >= g) return;
   pdl_wait();
-  const int b = blockIdx.x, lane = threadIdx.x & 31, head = blockIdx.y * 4 + (threadIdx.x >> 5);
-  const int4 rec = a.rec[b];
-  if (rec.x < 0) return;
-  const int g = a.h / a.h_kv, m = rec.y / a.groups, hg = rec.y - m * a.groups;
-  if (head >= min(HB, g - hg * HB)) return;
   // its parts: the second of block b, the first of the blocks behind it up to the one where it ends
+  int4 rec = make_int4(0, 0, 2, 0);
+  if (b + lane < gridDim.x) rec = __ldcg(a.rec + b + lane);
+  const int r = __shfl_sync(0xffffffffu, rec.x, 0), item = __shfl_sync(0xffffffffu, rec.y, 0);
+  if (r < 0) return;
+  const int m = item / a.groups, hg = item - m * a.groups;
+  if (head >= min(HB, g - hg * HB)) return;
   int n = 1;
-  for (int at = b + 1;; at += 32) {
-    const bool end = at + lane < gridDim.x ? a.rec[at + lane].z == 2 : true;
-    const unsigned ends = __ballot_sync(0xffffffffu, end);
-    if (ends) { n += at - b - 1 + __ffs(ends); break; }
+  for (int at = b;; at += 32) {
+    if (at > b) rec.z = at + lane < gridDim.x ? __ldcg(&a.rec[at + lane].z) : 2;
+    const unsigned ends = __ballot_sync(0xffffffffu, rec.z == 2 && at + lane > b);
+    if (ends) { n = at - b + __ffs(ends); break; }
   }
-  auto part = [&](int i) { return a.part + ((size_t)(b + i) * 2 + (i == 0 ? 1 : 0)) * (HB * (D + 2)); };
+  const float *const first = a.part + ((size_t)b * 2 + 1) * PART, *const others = a.part + (size_t)b * 2 * PART;   // (part i > 0)
+  auto part = [&](int i) { return i == 0 ? first : others + (size_t)i * 2 * PART; };
+  // this thread's columns of its first parts, on their way while the scale is found
+  const int slot = tid / TPP, c4 = tid - slot * TPP;
+  float4 o[JOIN_BATCH];
+  float2 ml[JOIN_BATCH];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < JOIN_BATCH; u++) {
+      const int i = i0 + u * AT_ONCE + slot;
+      o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      ml[u] = make_float2(-INFINITY, 0.f);
+      if (i < n && slot < AT_ONCE) {
+        o[u] = __ldcg(reinterpret_cast<const float4 *>(part(i) + head * D) + c4);
+        ml[u] = __ldcg(reinterpret_cast<const float2 *>(part(i) + HB * D) + head);
+      }
+    }
+  };
+  fetch(0);
   float top = -INFINITY;
-  for (int i = lane; i < n; i += 32) top = fmaxf(top, part(i)[HB * D + head * 2]);
+  for (int i = tid; i < n; i += JOIN_THREADS) top = fmaxf(top, __ldcg(part(i) + HB * D + head * 2));
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  if (lane == 0) tops[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < JOIN_THREADS / 32; w++) top = fmaxf(top, tops[w]);
   const float ref = top == -INFINITY ? 0.f : top;
-  float l = 0.f, acc[C] = {};
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    float w = 0.f;
-    if (i0 + lane < n) {
-      const float2 ml = *reinterpret_cast<const float2 *>(part(i0 + lane) + HB * D + head * 2);
-      w = exp2f(ml.x - ref);
-      l += w * ml.y;
-    }
-    const int count = min(32, n - i0);
-#pragma unroll 8
-    for (int i = 0; i < count; i++) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      const float *o = part(i0 + i) + head * D + lane;
+  float l = 0.f;   // (of this thread's parts, in column 0's threads)
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0;;) {
 #pragma unroll
-      for (int c = 0; c < C; c++) acc[c] = fmaf(wi, o[c * 32], acc[c]);
+    for (int u = 0; u < JOIN_BATCH; u++) {
+      const float w = exp2f(ml[u].x - ref);
+      acc.x = fmaf(w, o[u].x, acc.x); acc.y = fmaf(w, o[u].y, acc.y);
+      acc.z = fmaf(w, o[u].z, acc.z); acc.w = fmaf(w, o[u].w, acc.w);
+      l = fmaf(w, ml[u].y, l);
     }
+    i0 += JOIN_BATCH * AT_ONCE;
+    if (i0 >= n) break;
+    fetch(i0);
   }
+  if (slot < AT_ONCE) {
+    sums[slot][c4] = acc;
+    if (c4 == 0) ls[slot] = l;
+  }
+  __syncthreads();
+  if (tid >= TPP) return;
+  l = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+  for (int s = 0; s < AT_ONCE; s++) {
+    const float4 x = sums[s][tid];
+    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+    l += ls[s];
+  }
   const int j = m * g + hg * HB + head;
-  T *out = static_cast<T *>(a.out) + rec.x * a.out_req + j * a.out_head + lane;
-#pragma unroll
-  for (int c = 0; c < C; c++) {
-    const uint32_t v = Half2<T>::pack(acc[c] / l, 0.f);
-    *reinterpret_cast<uint16_t *>(out + c * 32) = (uint16_t)v;
-  }
-  if (a.lse && lane == 0) a.lse[(size_t)rec.x * a.h + j] = (top + log2f(l)) * 0.6931471805599453f;
+  const float inv = 1.0f / l;
+  *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + r * a.out_req + j * a.out_head + tid * 4) =
+      make_uint2(Half2<T>::pack(acc.x * inv, acc.y * inv), Half2<T>::pack(acc.z * inv, acc.w * inv));
+  if (a.lse && tid == 0) a.lse[(size_t)r * a.h + j] = (top + log2f(l)) * 0.6931471805599453f;
 }
 
 int heads_per_block(int h, int h_kv) { return h / h_kv > 8 ? 16 : 8; }
@@ -462,7 +500,7 @@ cudaError_t launch(const PagedAttn &a, cudaStream_t st) {
   const int blocks = paged_blocks();
   e = launch_kernel(paged_attn_kernel<T, D, NT>, dim3(blocks), dim3(PA_THREADS), S::BYTES, st, false, a);
   if (e != cudaSuccess) return e;
-  return launch_kernel(paged_join_kernel<T, D, NT>, dim3(blocks, NT * 2), dim3(128), 0, st, true, a);
+  return launch_kernel(paged_join_kernel<T, D, NT>, dim3(blocks, 8 * NT), dim3(JOIN_THREADS), 0, st, true, a);
 }
 
 template <typename T>

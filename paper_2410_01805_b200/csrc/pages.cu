@@ -13,7 +13,7 @@ namespace {
 // the sums for itself (at most LOCRET_MAX_REQUESTS lengths from L2), and the blocks share the entries and rows.  The one
 // barrier of the cluster stands between reading and writing: behind it lens_out and n_free_out may overwrite their inputs, and
 // pages that were pushed onto the list can be taken from it.
-constexpr int PS_THREADS = 512, PS_WARPS = PS_THREADS / 32, PS_MAX_BLOCKS = 8;
+constexpr int PS_THREADS = 512, PS_WARPS = PS_THREADS / 32, PS_MAX_BLOCKS = 8, PS_SHARE = 8;
 
 struct PagesStepArgs {
   int32_t *table;
@@ -21,33 +21,33 @@ struct PagesStepArgs {
   const int32_t *lens_in, *new_lens, *n_free_in;
   int32_t *lens_out, *free_pages, *n_free_out, *positions, *starts, *status;
   int64_t *slots;
-  int width, n_req, page_size, capacity, n_tok;
+  int width, n_req, page_size, capacity, n_tok, vec;   // vec: slots and positions are aligned for 16-byte stores
+  FastDiv by_page;
 };
 
-// Exclusive prefix sum over the block's threads of one 64-bit number each; *total is the whole sum.
-__device__ long long block_scan(long long v, long long *warp_sums, long long *total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
+// Exclusive prefix sums over the block's threads of two 64-bit numbers each; sum0, sum1 are the whole sums.
+__device__ void block_scan(long long &v0, long long &v1, long long &sum0, long long &sum1, longlong2 *warp_sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  auto warp_scan = [&](long long v) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();   // (the last call's readers of warp_sums are done)
-  if (lane == 31) warp_sums[warp] = x;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    return v;
+  };
+  const long long x0 = warp_scan(v0), x1 = warp_scan(v1);
+  if (lane == 31) warp_sums[warp] = make_longlong2(x0, x1);
   __syncthreads();
-  long long before = 0, sum = 0;
-#pragma unroll
-  for (int w = 0; w < PS_WARPS; w++) {
-    const long long s = warp_sums[w];
-    if (w < warp) before += s;
-    sum += s;
-  }
-  *total = sum;
-  return before + x - v;
+  const longlong2 mine = lane < warps ? warp_sums[lane] : make_longlong2(0, 0);
+  const long long w0 = warp_scan(mine.x), w1 = warp_scan(mine.y);
+  sum0 = __shfl_sync(0xffffffffu, w0, 31);
+  sum1 = __shfl_sync(0xffffffffu, w1, 31);
+  v0 = x0 - v0 + (warp ? __shfl_sync(0xffffffffu, w0, warp - 1) : 0);
+  v1 = x1 - v1 + (warp ? __shfl_sync(0xffffffffu, w1, warp - 1) : 0);
 }
 
-// The request whose range [first[r], first[r + 1]) holds i; 0 <= i < first[n].
+// The request whose range [first[r], first[r + 1]) holds i, 0 <= i, i < first[n] (which is not read).
 __device__ __forceinline__ int owner(const int *first, int n, int i) {
   int lo = 0, hi = n;   // first[lo] <= i < first[hi]
   while (hi - lo > 1) {
@@ -59,36 +59,39 @@ __device__ __forceinline__ int owner(const int *first, int n, int i) {
 
 constexpr int REFUSED = INT32_MIN;   // in place of a request's length
 
+// A thread's requests are its `per` ones from r0 on.  CLUSTER: several blocks (else the one needs no more than its own barriers).
+template <bool CLUSTER>
 __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_constant__ PagesStepArgs a) {
   extern __shared__ int ps_smem[];
   int *const starts = ps_smem, *const need0 = starts + a.n_req + 1, *const len = need0 + a.n_req + 1;
-  __shared__ long long warp_sums[PS_WARPS];
-  const int tid = threadIdx.x, rank = blockIdx.x, n_blocks = gridDim.x;
-  const int per = (a.n_req + PS_THREADS - 1) / PS_THREADS;
+  __shared__ longlong2 sums_a[PS_WARPS], sums_b[PS_WARPS];
+  __shared__ int taken;
+  const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, rank = CLUSTER ? blockIdx.x : 0, n_blocks = CLUSTER ? gridDim.x : 1;
+  const int per = (a.n_req + threads - 1) / threads;
   const int r0 = min(a.n_req, tid * per), r1 = min(a.n_req, r0 + per);
   const int page = a.page_size;
   const long long room = min((long long)a.width * page, (long long)INT32_MAX);
-  auto pages_of = [&](long long n) { return (int)((n + page - 1) / page); };   // (n <= room: fits)
+  auto pages_of = [&](int n) { return n ? a.by_page.div(n - 1) + 1 : 0; };
+  if (tid == 0) taken = 0;
 
   // rows of every request; pages that come back
-  long long rows = 0, back = 0, total_rows, total_back, total_need;
+  int n_free = *a.n_free_in;
+  long long row = 0, push = 0, total_rows, total_back;
   for (int r = r0; r < r1; r++) {
     const int n = a.lens_in[r], x = a.new_lens[r];
     const bool bad = n < 0 || n > room;
-    rows += max(x, 0);
-    if (x < 0 && !bad) back += pages_of(n);
+    row += max(x, 0);
+    if (x < 0 && !bad) push += pages_of(n);
     len[r] = bad ? REFUSED : n;
   }
-  int n_free = *a.n_free_in;
   const bool bad_list = n_free < 0 || n_free > a.capacity;
   n_free = min(max(n_free, 0), a.capacity);
-  long long row = block_scan(rows, warp_sums, &total_rows);
-  long long push = block_scan(back, warp_sums, &total_back);
+  block_scan(row, push, total_rows, total_back, sums_a);
   const bool too_many = n_free + total_back > a.capacity;   // (some page is on the list twice)
   const int top = (int)min(n_free + total_back, (long long)a.capacity);
 
   // who is refused before the list is looked at; pages the others need
-  long long need = 0;
+  long long want = 0, none = 0, total_need, total_none;
   int code = 0;
   for (int r = r0; r < r1; r++) {
     const int x = a.new_lens[r], n = len[r];
@@ -100,24 +103,31 @@ __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_con
         len[r] = REFUSED;
         code = min(code, LOCRET_ERR_CAPACITY);
       } else {
-        need += pages_of((long long)n + x) - pages_of(n);
+        want += pages_of(n + x) - pages_of(n);
       }
     }
     row += max(x, 0);
   }
-  long long want = block_scan(need, warp_sums, &total_need);
+  block_scan(want, none, total_need, total_none, sums_b);
+  int last = 0;   // pages taken: the requests that get theirs come before the first that does not
   for (int r = r0; r < r1; r++) {
     const int x = a.new_lens[r], n = len[r];
     need0[r] = (int)min(want, (long long)top);
     if (n == REFUSED || x <= 0) continue;
-    const int more = pages_of((long long)n + x) - pages_of(n);
+    const int more = pages_of(n + x) - pages_of(n);
     want += more;
-    if (more > 0 && want > top) {   // (and so is every later request that needs a page)
-      len[r] = REFUSED;
-      need0[r] = top;
-      code = min(code, LOCRET_ERR_CAPACITY);
+    if (more > 0) {
+      if (want > top) {   // (and so is every later request that needs a page)
+        len[r] = REFUSED;
+        need0[r] = top;
+        code = min(code, LOCRET_ERR_CAPACITY);
+      } else {
+        last = (int)want;
+      }
     }
   }
+  last = __reduce_max_sync(0xffffffffu, last);
+  if (lane == 0 && last) atomicMax(&taken, last);
   if (tid == 0) {
     starts[a.n_req] = (int)min(total_rows, (long long)INT32_MAX);
     if (bad_list || too_many) code = min(code, LOCRET_ERR_INVALID);
@@ -125,53 +135,45 @@ __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_con
   if (code && rank == 0) report(a.status, code);
 
   // ended requests: their pages onto the list, one warp for each request, over all blocks
-  for (int r = r0; __any_sync(0xffffffffu, r < r1); r++) {
-    int count = 0, at = 0;
-    if (r < r1 && a.new_lens[r] < 0 && len[r] != REFUSED) {
-      count = pages_of(len[r]);
-      at = (int)min(push, (long long)INT32_MAX);
-      push += count;
-    }
-    for (unsigned todo = __ballot_sync(0xffffffffu, count > 0); todo; todo &= todo - 1) {
-      const int src = __ffs(todo) - 1;
-      const int c = __shfl_sync(0xffffffffu, count, src), first = __shfl_sync(0xffffffffu, at, src),
-                rr = __shfl_sync(0xffffffffu, r, src);
-      for (int j = rank * 32 + (tid & 31); j < c; j += n_blocks * 32) {
-        const long long to = (long long)n_free + first + j;
-        if (to < a.capacity) a.free_pages[to] = a.table[rr * a.table_stride + j];
+  if (total_back)
+    for (int r = r0; __any_sync(0xffffffffu, r < r1); r++) {
+      int count = 0, at = 0;
+      if (r < r1 && a.new_lens[r] < 0 && len[r] != REFUSED) {
+        count = pages_of(len[r]);
+        at = (int)min(push, (long long)INT32_MAX);
+        push += count;
+      }
+      for (unsigned todo = __ballot_sync(0xffffffffu, count > 0); todo; todo &= todo - 1) {
+        const int src = __ffs(todo) - 1;
+        const int c = __shfl_sync(0xffffffffu, count, src), first = __shfl_sync(0xffffffffu, at, src),
+                  rr = __shfl_sync(0xffffffffu, r, src);
+        const int32_t *from = a.table + rr * a.table_stride;
+        for (int j0 = rank * 32 + lane; j0 < c; j0 += 4 * n_blocks * 32) {   // (four at a time on their way)
+          int32_t p[4];
+#pragma unroll
+          for (int u = 0; u < 4; u++) p[u] = j0 + u * n_blocks * 32 < c ? from[j0 + u * n_blocks * 32] : 0;
+#pragma unroll
+          for (int u = 0; u < 4; u++) {
+            const int j = j0 + u * n_blocks * 32;
+            const long long to = (long long)n_free + first + j;
+            if (j < c && to < a.capacity) a.free_pages[to] = p[u];
+          }
+        }
       }
     }
-  }
-  // Number of pages taken: the requests that get theirs come before the first that does not.
-  __shared__ int taken;
-  if (tid == 0) taken = 0;
-  __syncthreads();
-  {
-    int last = 0;
-    for (int r = r0; r < r1; r++)
-      if (len[r] != REFUSED && a.new_lens[r] > 0) {
-        const int more = pages_of((long long)len[r] + a.new_lens[r]) - pages_of(len[r]);
-        if (more > 0) last = max(last, need0[r] + more);
-      }
-    last = __reduce_max_sync(0xffffffffu, last);
-    if ((tid & 31) == 0) atomicMax(&taken, last);
-  }
-  __syncthreads();
-  const int n_taken = taken;
-  if (tid == 0) need0[a.n_req] = n_taken;
-  // a request behind the last one that takes pages begins where the list's part ends
-  for (int r = r0; r < r1; r++) need0[r] = min(need0[r], n_taken);
 
   // everything that is read has been read, and what was pushed can be seen
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (CLUSTER) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else __syncthreads();
 
-  for (int r = rank * PS_THREADS + tid; r < a.n_req; r += n_blocks * PS_THREADS) {
-    const int x = a.new_lens[r];
+  const int n_taken = taken;   // (need0 of a request behind the last that takes pages is no less)
+  for (int r = rank * threads + tid; r < a.n_req; r += n_blocks * threads) {
+    const int x = a.new_lens[r], n = len[r];
     a.starts[r] = starts[r];
-    if (len[r] == REFUSED) {
+    if (n == REFUSED) {
       if (a.lens_out != a.lens_in) a.lens_out[r] = a.lens_in[r];
     } else {
-      a.lens_out[r] = x < 0 ? 0 : len[r] + x;
+      a.lens_out[r] = x < 0 ? 0 : n + x;
     }
   }
   if (rank == 0 && tid == 0) {
@@ -179,29 +181,50 @@ __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_con
     *a.n_free_out = top - n_taken;
   }
   // the table's new entries
-  for (int k = rank * PS_THREADS + tid; k < n_taken; k += n_blocks * PS_THREADS) {
+  for (int k = rank * threads + tid; k < n_taken; k += n_blocks * threads) {
     const int r = owner(need0, a.n_req, k);
     a.table[r * a.table_stride + pages_of(len[r]) + k - need0[r]] = a.free_pages[top - 1 - k];
   }
-  // the rows
+  // the rows, four in a row for each thread (one search)
   const int n_rows = starts[a.n_req];
-  for (int t = rank * PS_THREADS + tid; t < a.n_tok; t += n_blocks * PS_THREADS) {
-    int64_t slot = -1;
-    int pos = 0;
-    if (t < n_rows) {
-      const int r = owner(starts, a.n_req, t), n = len[r];
-      if (n != REFUSED) {
-        pos = n + (t - starts[r]);
-        const int j = pos / page, old = pages_of(n);
-        const int p = j < old ? a.table[r * a.table_stride + j] : a.free_pages[top - 1 - (need0[r] + j - old)];
-        if (p >= 0 && p < a.capacity) slot = (int64_t)p * page + (pos - j * page);
-        else report(a.status, LOCRET_ERR_INVALID);
-      } else {
-        pos = (int)max(0LL, min((long long)a.lens_in[r] + (t - starts[r]), (long long)INT32_MAX));
+  for (long long t0 = 4ll * (rank * threads + tid); t0 < a.n_tok; t0 += 4ll * n_blocks * threads) {
+    const int count = (int)min(4ll, a.n_tok - t0);
+    int64_t slot[4];
+    int pos[4], p[4], off[4], r = t0 < n_rows ? owner(starts, a.n_req, (int)t0) : 0;
+#pragma unroll
+    for (int u = 0; u < 4; u++) {
+      const int t = (int)t0 + u;
+      slot[u] = -1;
+      pos[u] = p[u] = off[u] = 0;
+      if (u < count && t < n_rows) {
+        while (starts[r + 1] <= t) r++;   // (ends: t < n_rows = starts[n_req])
+        const int n = len[r], i = t - starts[r];
+        if (n != REFUSED) {
+          pos[u] = n + i;
+          const int j = a.by_page.div(pos[u]), old = pages_of(n);
+          off[u] = pos[u] - j * page;
+          p[u] = j < old ? a.table[r * a.table_stride + j] : a.free_pages[top - 1 - (need0[r] + j - old)];
+          slot[u] = 0;
+        } else {
+          pos[u] = (int)max(0LL, min((long long)a.lens_in[r] + i, (long long)INT32_MAX));
+        }
       }
     }
-    a.slots[t] = slot;
-    a.positions[t] = pos;
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+      if (slot[u] == 0) {
+        if (p[u] >= 0 && p[u] < a.capacity) slot[u] = (int64_t)p[u] * page + off[u];
+        else { slot[u] = -1; report(a.status, LOCRET_ERR_INVALID); }
+      }
+    if (count == 4 && a.vec) {
+      reinterpret_cast<longlong2 *>(a.slots + t0)[0] = make_longlong2(slot[0], slot[1]);
+      reinterpret_cast<longlong2 *>(a.slots + t0)[1] = make_longlong2(slot[2], slot[3]);
+      *reinterpret_cast<int4 *>(a.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; u++)
+        if (u < count) { a.slots[t0 + u] = slot[u]; a.positions[t0 + u] = pos[u]; }
+    }
   }
 }
 
@@ -215,10 +238,10 @@ export_pages_kernel(const bf16 *__restrict__ k_rot, const bf16 *__restrict__ v, 
   if (x >= (long long)len * per_row) return;
   const int i = (int)(x / per_row), c = ((int)(x - (long long)i * per_row)) * 8;
   const int pos = i < ranked_len ? rank[(size_t)m * cap + i] : i;
-  const int p = pos >= 0 && pos < len ? table[pos / pg.page_size] : -1;
+  const int j = pg.by_size.div(pos), p = pos >= 0 && pos < len ? table[j] : -1;
   if (p < 0 || p >= pg.n_pages) { report(status, LOCRET_ERR_INVALID); return; }
   const size_t src = ((size_t)m * cap + i) * d + c;
-  const long long dst = p * pg.page_stride + m * pg.head_stride + (pos % pg.page_size) * pg.token_stride + c;
+  const long long dst = p * pg.page_stride + m * pg.head_stride + (pos - j * pg.page_size) * pg.token_stride + c;
   *reinterpret_cast<uint4 *>(static_cast<bf16 *>(pg.k) + dst) = *reinterpret_cast<const uint4 *>(k_rot + src);
   *reinterpret_cast<uint4 *>(static_cast<bf16 *>(pg.v) + dst) = *reinterpret_cast<const uint4 *>(v + src);
 }
@@ -245,20 +268,23 @@ extern "C" int locret_pages_step(int32_t *table, int64_t table_stride, int32_t w
     return LOCRET_ERR_INVALID;
   if (!free_pages || !n_free_in || !n_free_out || !starts || (n_tok && (!slots || !positions))) return LOCRET_ERR_INVALID;
   if (n_req && (!table || !lens_in || !lens_out || !new_lens || (n_req > 1 && table_stride < width))) return LOCRET_ERR_INVALID;
+  const int vec = ((reinterpret_cast<uintptr_t>(slots) | reinterpret_cast<uintptr_t>(positions)) & 15u) == 0;
   const PagesStepArgs a = {table, table_stride, lens_in, new_lens, n_free_in, lens_out, free_pages, n_free_out, positions,
-                           starts, status, slots, width, n_req, page_size, capacity, n_tok};
-  cudaLaunchConfig_t cfg = {};
-  const int work = n_tok > n_req ? n_tok : n_req;
-  int blocks = 1;   // (a power of two, so that clusters of it exist)
-  while (blocks < PS_MAX_BLOCKS && blocks * PS_THREADS < work) blocks *= 2;
+                           starts, status, slots, width, n_req, page_size, capacity, n_tok, vec, FastDiv(page_size)};
+  // One block where a thread has no more than a request and four rows to do, and no wider than that needs; else a cluster.
+  const int per_thread = n_tok / 4 > PS_SHARE * n_req ? n_tok / 4 + 1 : PS_SHARE * n_req;
+  int threads = 128, blocks = 1;
+  while (threads < PS_THREADS && threads < per_thread) threads *= 2;
+  while (blocks < PS_MAX_BLOCKS && blocks * threads < per_thread) blocks *= 2;
   const size_t smem = sizeof(int) * (3 * (size_t)n_req + 2);
   static PerDeviceFlag flag;
-  if (allow_dynamic_smem(pages_step_kernel, (int)sizeof(int) * (3 * LOCRET_MAX_REQUESTS + 2), flag) != cudaSuccess) {
+  if (allow_dynamic_smem(pages_step_kernel<true>, (int)sizeof(int) * (3 * LOCRET_MAX_REQUESTS + 2), flag) != cudaSuccess) {
     cudaGetLastError();
     return LOCRET_ERR_CUDA;
   }
+  cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(PS_THREADS);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = (cudaStream_t)stream;
   cudaLaunchAttribute attr[1];
@@ -266,7 +292,10 @@ extern "C" int locret_pages_step(int32_t *table, int64_t table_stride, int32_t w
   attr[0].val.clusterDim.x = blocks;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, pages_step_kernel, a) != cudaSuccess) { cudaGetLastError(); return LOCRET_ERR_CUDA; }
+  cfg.numAttrs = blocks > 1 ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, blocks > 1 ? pages_step_kernel<true> : pages_step_kernel<false>, a) != cudaSuccess) {
+    cudaGetLastError();
+    return LOCRET_ERR_CUDA;
+  }
   return LOCRET_OK;
 }
