@@ -451,7 +451,8 @@ enum { LOCRET_BF16 = 0, LOCRET_FP16 = 1 };   /* dtype arguments */
 #define LOCRET_MAX_REQUESTS 4096             /* requests in one call */
 
 /* One layer's pool.  Column c of the key of token i of KV head m in page p: k + p * page_stride + m * head_stride +
- * i * token_stride + c, in elements; values likewise.  Pointers 16-byte aligned, strides multiples of 8 and >= 0. */
+ * i * token_stride + c, in elements; values likewise.  Pointers 16-byte aligned, strides multiples of 8 and >= 0.  locret_paged_attention takes
+ * pools whose keys (and values) lie within 64 GiB. */
 typedef struct {
   void *k, *v;
   int32_t n_pages, page_size, n_kv_heads, head_dim;   /* page_size: tokens per page, any number >= 1 */

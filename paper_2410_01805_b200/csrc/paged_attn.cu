@@ -2,7 +2,7 @@
 //
 // Bound by memory: every visible key and value is read once, 4 d bytes of each for 4 g d operations.  So the kernel is a
 // stream of asynchronous copies with the arithmetic hidden behind it:
-//  * The visible keys of every (request, KV head) are cut into steps of 64, and all steps of the batch, one after the other,
+//  * The visible keys of every (request, KV head) are cut into steps (16 per warp), and all steps of the batch, one after the other,
 //    form a line that is cut into equal parts, one for each block of a persistent grid: lengths may differ as they like, and
 //    one long request fills the GPU as well as many short ones.  Every block finds its part by summing the lengths itself.
 //  * A warp takes 16 keys of each step and has a ring of stages of its own, filled by its own copies: no barrier of the block
@@ -21,7 +21,12 @@
 namespace locret {
 namespace {
 
-constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32, PA_STEP = PA_WARPS * 16, PA_STAGES = 3, PA_PER_SM = 2;
+// Warps of a block, stages of a warp's ring, blocks of an SM.  What the loop waits for is its own chain of instructions, so more
+// warps do more than more stages, as far as shared memory and registers go.
+template <int D, int NT> struct PaCfg { static constexpr int WARPS = 4, STAGES = 3, PER_SM = 2; static constexpr bool TWO = false; };
+template <> struct PaCfg<128, 1> { static constexpr int WARPS = 5, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
+template <> struct PaCfg<96, 1> { static constexpr int WARPS = 5, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
+template <> struct PaCfg<64, 1> { static constexpr int WARPS = 7, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
 constexpr float PA_RAISE = 8.0f;   // log2 of how far a score may exceed the running scale
 
 template <typename T>
@@ -42,6 +47,12 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   return d;
 }
 
+__device__ __forceinline__ float exp2_fast(float x) {   // (results below 2^-126 are 0)
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 struct PagedAttn {
   const void *q;
   void *out;
@@ -50,7 +61,10 @@ struct PagedAttn {
                            // item, z = 1 if the block's first part goes on behind it, 2 if it ends there (0: none)
   const int32_t *table, *lens;
   int32_t *status;
-  PageView pages;
+  const uint4 *k, *v;      // the pool; places in it in units of 16 bytes, 32 bits (one exchange and one product instead of several)
+  uint32_t page_stride, head_stride, token_stride;
+  int n_pages, page_size;
+  FastDiv by_size;
   long long q_req, q_head, out_req, out_head, table_stride;
   int width, n_req, h, h_kv, groups, window, sinks;   // groups: blocks of heads per KV head
   float scale_log2;
@@ -60,11 +74,11 @@ struct PagedAttn {
 struct Visible {
   int n, shift, sinks;
   __device__ __forceinline__ int key(int i) const { return i < sinks ? i : i + shift; }
-  __device__ __forceinline__ int steps() const { return n > 0 ? (n - 1) / PA_STEP + 1 : 1; }   // (an empty request has one, to write zeros)
+  template <int STEP> __device__ __forceinline__ int steps() const { return n > 0 ? (n - 1) / STEP + 1 : 1; }   // (an empty request has one, to write zeros)
 };
 __device__ __forceinline__ int clamped_len(const PagedAttn &a, int r) {
   const int n = __ldg(a.lens + r);
-  return max(0, (int)min((long long)n, (long long)a.width * a.pages.page_size));
+  return max(0, (int)min((long long)n, (long long)a.width * a.page_size));
 }
 __device__ __forceinline__ Visible visible_of(const PagedAttn &a, int len) {
   Visible v = {len, 0, 0};
@@ -77,36 +91,54 @@ __device__ __forceinline__ Visible visible_of(const PagedAttn &a, int len) {
   return v;
 }
 
-// A place in the line: step `tile` of item `item` (KV head, block of heads) of request r.
+// A place in the line: step `tile` of KV head m and block of heads hg of request r.
+template <int STEP>
 struct Cursor {
-  int r, item, tile, steps;
+  int r, m, hg, tile, steps, next_len;   // next_len: of the request behind, on its way
+  uint32_t head_at;                      // where head m begins in a page
+  const int32_t *row;                    // the request's pages
   Visible v;
-  __device__ __forceinline__ void enter(const PagedAttn &a, int request) {
+  __device__ __forceinline__ void enter(const PagedAttn &a, int request, int len) {
     r = request;
-    v = visible_of(a, clamped_len(a, min(r, a.n_req - 1)));
-    steps = v.steps();
+    m = hg = tile = 0;
+    head_at = 0;
+    row = a.table + r * a.table_stride;
+    v = visible_of(a, len);
+    steps = v.template steps<STEP>();
+    next_len = clamped_len(a, min(r + 1, a.n_req - 1));
   }
-  __device__ __forceinline__ void next(const PagedAttn &a, int items) {
+  __device__ __forceinline__ void next(const PagedAttn &a) {
     if (++tile < steps) return;
     tile = 0;
-    if (++item < items) return;
-    item = 0;
-    enter(a, r + 1);
+    if (++hg < a.groups) return;
+    hg = 0;
+    head_at += a.head_stride;
+    if (++m < a.h_kv) return;
+    enter(a, r + 1, next_len);
   }
 };
+// (m, hg) in one word, for the records
+__device__ __forceinline__ int pack_item(int m, int hg) { return (int)((uint32_t)m | (uint32_t)hg << 16); }
+__device__ __forceinline__ int item_m(int item) { return item & 0xffff; }
+__device__ __forceinline__ int item_hg(int item) { return (int)((uint32_t)item >> 16); }
 
 // The block's part [lo, hi) of the line, the request in which it begins, and how far into the request (in steps of all its
 // items).  With fewer steps than blocks the first blocks take one each, so that no block between two parts of an item is empty.
+template <int WARPS>
 __device__ void find(const PagedAttn &a, int items, long long &lo, long long &hi, int &r_out, long long &into) {
-  __shared__ long long warp_sums[PA_WARPS], found_into;
+  constexpr int STEP = WARPS * 16, THREADS = WARPS * 32;
+  __shared__ long long warp_sums[WARPS], found_into;
   __shared__ int found_r;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (a.n_req + PA_THREADS - 1) / PA_THREADS, r0 = min(a.n_req, tid * per), r1 = min(a.n_req, r0 + per);
+  // every warp by itself for up to 32 requests, else the block
+  const bool few = a.n_req <= 32;
+  const int at = few ? lane : tid, per = few ? 1 : (a.n_req + THREADS - 1) / THREADS;
+  const int r0 = min(a.n_req, at * per), r1 = min(a.n_req, r0 + per);
   long long mine = 0;
   for (int r = r0; r < r1; r++) {
     const int raw = __ldg(a.lens + r), len = clamped_len(a, r);
     if (raw != len && blockIdx.x == 0) report(a.status, LOCRET_ERR_INVALID);
-    mine += visible_of(a, len).steps();
+    mine += visible_of(a, len).template steps<STEP>();
   }
   long long x = mine;
 #pragma unroll
@@ -114,23 +146,33 @@ __device__ void find(const PagedAttn &a, int items, long long &lo, long long &hi
     const long long y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  if (lane == 31) warp_sums[warp] = x;
-  __syncthreads();
-  long long before = x - mine, total = 0;
+  long long before = x - mine, total = __shfl_sync(0xffffffffu, x, 31);
+  if (!few) {
+    if (lane == 31) warp_sums[warp] = x;
+    __syncthreads();
+    total = 0;
 #pragma unroll
-  for (int w = 0; w < PA_WARPS; w++) {
-    if (w < warp) before += warp_sums[w];
-    total += warp_sums[w];
+    for (int w = 0; w < WARPS; w++) {
+      if (w < warp) before += warp_sums[w];
+      total += warp_sums[w];
+    }
   }
   total *= items;
   const long long parts = min((long long)gridDim.x, total), part = min((long long)blockIdx.x, parts);
   lo = total * part / parts;
   hi = part < parts ? total * (part + 1) / parts : lo;
-  if (lo < hi && before * items <= lo && lo < (before + mine) * items) {
+  const bool here = lo < hi && before * items <= lo && lo < (before + mine) * items;
+  if (few) {
+    const int src = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+    r_out = max(src, 0);
+    into = lo - __shfl_sync(0xffffffffu, before, r_out) * items;
+    return;
+  }
+  if (here) {
     long long rest = lo - before * items;
     int r = r0;
     for (; r < r1; r++) {
-      const long long n = (long long)visible_of(a, clamped_len(a, r)).steps() * items;
+      const long long n = (long long)visible_of(a, clamped_len(a, r)).template steps<STEP>() * items;
       if (rest < n) break;
       rest -= n;
     }
@@ -146,115 +188,152 @@ template <typename T, int D, int NT>
 struct PaSmem {
   static constexpr int LD = D + 8, HB = 8 * NT, LF = D / 2 + 4;   // (rows of both spread over the banks)
   static constexpr int STAGE = 2 * 16 * LD * 2;                   // bytes: keys and values of a warp's 16
-  static constexpr int BYTES = PA_WARPS * PA_STAGES * STAGE + PA_WARPS * 8 * LF * 4;
+  typedef PaCfg<D, NT> Cfg;
+  static constexpr int FO = Cfg::WARPS * 8 * LF;                  // floats in which the warps meet
+  static constexpr int BYTES = Cfg::WARPS * Cfg::STAGES * STAGE + (Cfg::TWO ? 2 : 1) * FO * 4;
+  static_assert(Cfg::PER_SM * (BYTES + 2500) <= 228 * 1024, "blocks of an SM");
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const __grid_constant__ PagedAttn a) {
+__global__ void __launch_bounds__(PaCfg<D, NT>::WARPS * 32, PaCfg<D, NT>::PER_SM)
+paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   using S = PaSmem<T, D, NT>;
-  constexpr int LD = S::LD, HB = S::HB, LF = S::LF, VPR = D / 8, KD = D / 16;
+  constexpr int PA_WARPS = PaCfg<D, NT>::WARPS, PA_STAGES = PaCfg<D, NT>::STAGES, PA_THREADS = PA_WARPS * 32, PA_STEP = PA_WARPS * 16;
+  constexpr int LD = S::LD, HB = S::HB, LF = S::LF, KD = D / 16;
   extern __shared__ __align__(16) unsigned char pa_smem[];
-  __shared__ uint32_t there[PA_WARPS][PA_STAGES];                 // which of a stage's 16 keys exist
-  __shared__ float wm[PA_WARPS][HB], wl[PA_WARPS][HB];
+  __shared__ int4 info[PA_WARPS][PA_STAGES];
+  __shared__ float wm[2][PA_WARPS][HB], wl[2][PA_WARPS][HB];   // (two sets: one may still be read while the next is written)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g4 = lane >> 2, q4 = lane & 3;
-  const int g = a.h / a.h_kv, items = a.h_kv * a.groups;
+  const int items = a.h_kv * a.groups;
   T *const ring = reinterpret_cast<T *>(pa_smem + warp * PA_STAGES * S::STAGE);
-  float *const fo = reinterpret_cast<float *>(pa_smem + PA_WARPS * PA_STAGES * S::STAGE);   // [warp][8][LF]
+  float *const fo0 = reinterpret_cast<float *>(pa_smem + PA_WARPS * PA_STAGES * S::STAGE);   // [warp][8][LF], once or twice
+  using Cfg = PaCfg<D, NT>;
   pdl_launch_dependents();
 
   long long lo, hi, into;
   int r_first;
-  find(a, items, lo, hi, r_first, into);
+  find<PA_WARPS>(a, items, lo, hi, r_first, into);
   int4 rec = make_int4(-1, 0, 0, 0);
   if (lo >= hi) {
     if (tid == 0) a.rec[blockIdx.x] = rec;
     return;
   }
-  const long long n_steps = hi - lo;
+  const int n_steps = (int)(hi - lo);   // (the host refuses calls that could have more)
 
-  Cursor use;
-  use.enter(a, r_first);
-  use.item = (int)(into / use.steps);
-  use.tile = (int)(into - (long long)use.item * use.steps);
-  Cursor load = use;
+  Cursor<PA_STEP> load;
+  load.enter(a, r_first, clamped_len(a, r_first));
+  {
+    const int item = (int)(into / load.steps);
+    load.tile = (int)(into - (long long)item * load.steps);
+    load.m = item / a.groups;
+    load.hg = item - load.m * a.groups;
+    load.head_at = load.m * a.head_stride;
+  }
 
-  // where the rows of the next step to be requested lie: lane (and lane + 16) = row of the warp's 16
-  long long row_at = 0;
+  // The next step to be requested: lane (and lane + 16) = row of the warp's 16.  Its table entry is on its way a step ahead of its
+  // use.  A row is copied by as many neighbouring lanes as it has pieces of 16 bytes (a row in four pieces of 64 bytes, at fixed
+  // offsets from one address per lane, or a bulk copy per row, take fewer instructions and 10 and 30% more time).
+  constexpr int VPR = D / 8, COPIES = 16 * VPR / 32;
+  int row_page = 0, row_j = 0, row_key = 0;
   bool row_there = false;
   auto look_up = [&]() {
     const int i = load.tile * PA_STEP + warp * 16 + (lane & 15);
     row_there = i < load.v.n;
-    const int key = row_there ? load.v.key(i) : 0, j = a.pages.by_size.div(key);
-    const int page = row_there ? __ldg(a.table + load.r * a.table_stride + j) : 0;
-    if (page < 0 || page >= a.pages.n_pages) {
+    row_key = row_there ? load.v.key(i) : 0;
+    row_j = a.by_size.div(row_key);
+    row_page = row_there ? __ldg(load.row + row_j) : 0;
+  };
+  auto request = [&](int stage) {
+    if (row_page < 0 || row_page >= a.n_pages) {
       row_there = false;
       report(a.status, LOCRET_ERR_INVALID);
     }
-    const int m = load.item / a.groups;
-    row_at = row_there ? page * a.pages.page_stride + m * a.pages.head_stride + (key - j * a.pages.page_size) * a.pages.token_stride : 0;
-  };
-  auto request = [&](int stage) {
-    T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
     const uint32_t mask = __ballot_sync(0xffffffffu, row_there) & 0xffffu;
-    if (lane == 0) there[warp][stage] = mask;
+    const uint32_t at = row_there ? row_page * a.page_stride + (row_key - row_j * a.page_size) * a.token_stride + load.head_at : 0;
+    // what the step is, for the warp that will work on it: keys that exist | last of its item, request, item, step of the item
+    if (lane == 0) info[warp][stage] = make_int4((int)mask | (load.tile + 1 == load.steps ? 1 << 16 : 0) | (load.v.n > 0 ? 1 << 17 : 0),
+                                                 load.r, pack_item(load.m, load.hg), load.tile);
+    T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
 #pragma unroll
-    for (int x = 0; x < 16 * VPR / 32; x++) {
-      const int c = x * 32 + lane, row = c / VPR, col = (c - row * VPR) * 8;
-      const long long at = __shfl_sync(0xffffffffu, row_at, row) + col;
-      const bool ok = (mask >> row) & 1;
-      cp_async16(ks + row * LD + col, static_cast<const T *>(a.pages.k) + at, ok);
-      cp_async16(vs + row * LD + col, static_cast<const T *>(a.pages.v) + at, ok);
+    for (int x = 0; x < COPIES; x++) {
+      const int c = x * 32 + lane, row = c / VPR, col = c - row * VPR;
+      const uint32_t piece = __shfl_sync(0xffffffffu, at, row) + col;
+      const bool ok = mask == 0xffff || (mask >> row & 1);
+      cp_async16(ks + row * LD + col * 8, a.k + piece, ok);
+      cp_async16(vs + row * LD + col * 8, a.v + piece, ok);
     }
   };
-  long long asked = 0;
+  int to_ask = n_steps;
   look_up();
 #pragma unroll
   for (int s = 0; s < PA_STAGES - 1; s++) {
-    if (asked < n_steps) {
+    if (to_ask > 0) {
       request(s);
-      load.next(a, items);
-      if (++asked < n_steps) look_up();
+      load.next(a);
+      if (--to_ask > 0) look_up();
     }
     cp_async_commit();
   }
 
-  uint32_t qf[NT][KD][2];
+  const int g = a.h / a.h_kv;
+  auto load_q = [&](uint32_t (&to)[NT][KD][2], int r, int m, int hg) {
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+      const int head = hg * HB + nt * 8 + g4;   // within the group
+      const T *row = static_cast<const T *>(a.q) + r * a.q_req + (m * g + min(head, g - 1)) * a.q_head + q4 * 2;
+#pragma unroll
+      for (int kk = 0; kk < KD; kk++) {
+        to[nt][kk][0] = head < g ? *reinterpret_cast<const uint32_t *>(row + kk * 16) : 0u;
+        to[nt][kk][1] = head < g ? *reinterpret_cast<const uint32_t *>(row + kk * 16 + 8) : 0u;
+      }
+    }
+  };
+  uint32_t qf[NT][KD][2], qn[NT][KD][2];
+  bool first_item = true;
+  int set = 0;
   float o[NT][KD][4], m_run[NT][2], l_run[NT][2];
-  bool fresh = true;      // the state below belongs to no item yet
+  float m_ref[NT][2], m_most[NT][2];   // the scale as it is subtracted (0 for -inf), and what a score may not exceed
+  bool fresh = true;                   // the state belongs to no item yet
   int first_tile = 0, stage = 0;
-  for (long long step = 0; step < n_steps; step++) {
+  for (int left = n_steps; left > 0; left--) {
+    cp_async_wait<PA_STAGES - 2>();
+    __syncwarp();   // the other lanes' copies too; and all lanes are done with the stage that is refilled now
+    const int4 step = info[warp][stage];
     if (fresh) {
       fresh = false;
-      first_tile = use.tile;
-      const int m = use.item / a.groups, hg = use.item - m * a.groups;
+      first_tile = step.w;
+      const int m = item_m(step.z), hg = item_hg(step.z);
+      // the item's queries, requested when the last one began, and the next one's
+      if (first_item) load_q(qn, step.y, m, hg);
+      first_item = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int kk = 0; kk < KD; kk++) { qf[nt][kk][0] = qn[nt][kk][0]; qf[nt][kk][1] = qn[nt][kk][1]; }
+      const bool next_head = hg + 1 == a.groups, next_r = next_head && m + 1 == a.h_kv;
+      load_q(qn, min(next_r ? step.y + 1 : step.y, a.n_req - 1), next_r ? 0 : next_head ? m + 1 : m, next_head ? 0 : hg + 1);
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
-        const int head = hg * HB + nt * 8 + g4;   // within the group
-        const T *row = static_cast<const T *>(a.q) + use.r * a.q_req + (m * g + min(head, g - 1)) * a.q_head + q4 * 2;
-#pragma unroll
-        for (int kk = 0; kk < KD; kk++) {
-          qf[nt][kk][0] = head < g ? *reinterpret_cast<const uint32_t *>(row + kk * 16) : 0u;
-          qf[nt][kk][1] = head < g ? *reinterpret_cast<const uint32_t *>(row + kk * 16 + 8) : 0u;
-        }
 #pragma unroll
         for (int kk = 0; kk < KD; kk++)
 #pragma unroll
           for (int e = 0; e < 4; e++) o[nt][kk][e] = 0.f;
-        m_run[nt][0] = m_run[nt][1] = -INFINITY;
-        l_run[nt][0] = l_run[nt][1] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          m_run[nt][e] = m_most[nt][e] = -INFINITY;
+          m_ref[nt][e] = l_run[nt][e] = 0.f;
+        }
       }
     }
-    cp_async_wait<PA_STAGES - 2>();
-    __syncwarp();   // the other lanes' copies too; and all lanes are done with the stage that is refilled now
-    if (asked < n_steps) {
+    if (to_ask > 0) {
       request(stage == 0 ? PA_STAGES - 1 : stage - 1);   // (the stage of the last step)
-      load.next(a, items);
-      if (++asked < n_steps) look_up();
+      load.next(a);
+      if (--to_ask > 0) look_up();
     }
     cp_async_commit();
 
     const T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
-    const uint32_t mask = there[warp][stage];
+    const uint32_t mask = step.x & 0xffff;
     if (mask) {
       float s[NT][4] = {};
 #pragma unroll
@@ -265,14 +344,22 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
         for (int nt = 0; nt < NT; nt++) mma16<T>(s[nt], a0, a1, a2, a3, qf[nt][kk][0], qf[nt][kk][1]);
       }
       // s[nt]: keys g4, g4, g4 + 8, g4 + 8 of heads 2 q4, 2 q4 + 1, 2 q4, 2 q4 + 1
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) s[nt][e] *= a.scale_log2;
+      if (mask != 0xffff) {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (!((mask >> (g4 + (e >> 1) * 8)) & 1)) s[nt][e] = -INFINITY;
+      }
       bool raise = false;
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          s[nt][e] = (mask >> (g4 + (e >> 1) * 8)) & 1 ? s[nt][e] * a.scale_log2 : -INFINITY;
-          raise |= s[nt][e] > m_run[nt][e & 1] + PA_RAISE;
-        }
+        for (int e = 0; e < 4; e++) raise |= s[nt][e] > m_most[nt][e & 1];
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
@@ -283,7 +370,9 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
             const float top = fmaxf(m_run[nt][e], t);
-            alpha[e] = exp2f(m_run[nt][e] - (top == -INFINITY ? 0.f : top));
+            m_ref[nt][e] = top == -INFINITY ? 0.f : top;
+            m_most[nt][e] = top + PA_RAISE;
+            alpha[e] = exp2_fast(m_run[nt][e] - m_ref[nt][e]);
             m_run[nt][e] = top;
             l_run[nt][e] *= alpha[e];
           }
@@ -302,8 +391,7 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
           float p[2];
 #pragma unroll
           for (int e = 0; e < 2; e++) {
-            const float m = m_run[nt][e];
-            p[e] = exp2f(s[nt][half * 2 + e] - (m == -INFINITY ? 0.f : m));
+            p[e] = exp2_fast(s[nt][half * 2 + e] - m_ref[nt][e]);
             l_run[nt][e] += p[e];
           }
           const uint32_t hi16 = Half2<T>::pack(p[0], p[1]);
@@ -324,73 +412,68 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
     }
     __syncwarp();
 
-    const bool ends = use.tile + 1 == use.steps;
-    if (ends || step + 1 == n_steps) {
-      // ---- the warps meet
+    const bool ends = step.x >> 16 & 1;
+    if (ends || left == 1) {
+      // ---- the warps meet: each leaves its sums as they are, and who adds them up weighs them by their scales
       const bool whole = ends && first_tile == 0, begins = first_tile == 0;
-      const int m = use.item / a.groups, hg = use.item - m * a.groups, gh = min(HB, g - hg * HB);
+      const bool any = step.x >> 17 & 1;   // (a request of length 0: zeros)
+      const int m = item_m(step.z), hg = item_hg(step.z), gh = min(HB, g - hg * HB);
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
 #pragma unroll
         for (int e = 0; e < 2; e++) {
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) l_run[nt][e] += __shfl_xor_sync(0xffffffffu, l_run[nt][e], x);
-          if (g4 == 0) { wm[warp][nt * 8 + q4 * 2 + e] = m_run[nt][e]; wl[warp][nt * 8 + q4 * 2 + e] = l_run[nt][e]; }
+          if (g4 == 0) { wm[set][warp][nt * 8 + q4 * 2 + e] = m_run[nt][e]; wl[set][warp][nt * 8 + q4 * 2 + e] = l_run[nt][e]; }
         }
-      __syncthreads();
       float *const part = a.part + ((size_t)blockIdx.x * 2 + (begins ? 1 : 0)) * (HB * (D + 2));
 #pragma unroll
-      for (int nt = 0; nt < NT; nt++) {
-        float w[2];
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const int c = nt * 8 + q4 * 2 + e;
-          const float top = fmaxf(fmaxf(wm[0][c], wm[1][c]), fmaxf(wm[2][c], wm[3][c]));
-          w[e] = exp2f(m_run[nt][e] - (top == -INFINITY ? 0.f : top));
-        }
+      for (int nt = 0; nt < NT; nt++)
 #pragma unroll
         for (int side = 0; side < 2; side++) {
+          // two buffers: of a side's, every read was done before the barrier of the other; one: wait for the reads
+          if (!Cfg::TWO) __syncthreads();
+          float *const fo = fo0 + (Cfg::TWO ? side * S::FO : 0);
 #pragma unroll
           for (int kk = 0; kk < KD / 2; kk++)
 #pragma unroll
             for (int e = 0; e < 4; e++)
-              fo[(warp * 8 + q4 * 2 + (e & 1)) * LF + kk * 16 + g4 + (e >> 1) * 8] = o[nt][side * (KD / 2) + kk][e] * w[e & 1];
+              fo[(warp * 8 + q4 * 2 + (e & 1)) * LF + kk * 16 + g4 + (e >> 1) * 8] = o[nt][side * (KD / 2) + kk][e];
           __syncthreads();
           for (int x = tid; x < 8 * (D / 8); x += PA_THREADS) {   // (head, four columns of this half)
             const int hh = x / (D / 8), c = (x - hh * (D / 8)) * 4, head = nt * 8 + hh, col = side * (D / 2) + c;
             if (head >= gh) continue;
-            float top = wm[0][head], l = 0.f;
+            float top = wm[set][0][head], l = 0.f;
 #pragma unroll
-            for (int v = 1; v < PA_WARPS; v++) top = fmaxf(top, wm[v][head]);
+            for (int v = 1; v < PA_WARPS; v++) top = fmaxf(top, wm[set][v][head]);
             const float ref = top == -INFINITY ? 0.f : top;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int v = 0; v < PA_WARPS; v++) {
+              const float w = exp2_fast(wm[set][v][head] - ref);
               const float4 f = *reinterpret_cast<const float4 *>(fo + (v * 8 + hh) * LF + c);
-              sum.x += f.x; sum.y += f.y; sum.z += f.z; sum.w += f.w;
-              l += wl[v][head] * exp2f(wm[v][head] - ref);
+              sum.x = fmaf(w, f.x, sum.x); sum.y = fmaf(w, f.y, sum.y); sum.z = fmaf(w, f.z, sum.z); sum.w = fmaf(w, f.w, sum.w);
+              l = fmaf(w, wl[set][v][head], l);
             }
             const int j = m * g + hg * HB + head;
             if (whole) {
-              const float inv = use.v.n > 0 ? 1.0f / l : 0.f;
-              *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + use.r * a.out_req + j * a.out_head + col) =
+              const float inv = any ? 1.0f / l : 0.f;
+              *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + step.y * a.out_req + j * a.out_head + col) =
                   make_uint2(Half2<T>::pack(sum.x * inv, sum.y * inv), Half2<T>::pack(sum.z * inv, sum.w * inv));
-              if (a.lse && col == 0) a.lse[(size_t)use.r * a.h + j] = use.v.n > 0 ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
+              if (a.lse && col == 0) a.lse[(size_t)step.y * a.h + j] = any ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
             } else {
               *reinterpret_cast<float4 *>(part + head * D + col) = sum;
               if (col == 0) *reinterpret_cast<float2 *>(part + HB * D + head * 2) = make_float2(top, l);
             }
           }
-          __syncthreads();
         }
-      }
+      set ^= 1;
       if (!whole) {
-        if (begins) { rec.x = use.r; rec.y = use.item; }
+        if (begins) { rec.x = step.y; rec.y = step.z; }
         else rec.z = ends ? 2 : 1;
       }
       fresh = true;
     }
-    use.next(a, items);
     stage = stage + 1 == PA_STAGES ? 0 : stage + 1;
   }
   cp_async_wait<0>();
@@ -398,26 +481,24 @@ __global__ void __launch_bounds__(PA_THREADS, PA_PER_SM) paged_attn_kernel(const
 }
 
 // Block (b, head) joins that head of the item that begins in block b's part of the line and ends in another's.  A chain of
-// latencies (records, then parts): a thread takes four columns of every JOIN_AT_ONCE-th part and requests JOIN_BATCH of them
-// before it uses one (one 6000-token request, 38 parts an item: 22.9 us with a warp per head and a part after the other).
-constexpr int JOIN_THREADS = 128, JOIN_BATCH = 8;
+// latencies (records, then parts): a warp's lanes take four columns each, and JOIN_WARPS * JOIN_BATCH parts are requested before
+// one is used (one request of 6000 tokens, 38 parts an item: 23 us with a warp per head and a part after the other).
+constexpr int JOIN_WARPS = 4, JOIN_BATCH = 10;
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const __grid_constant__ PagedAttn a) {
-  constexpr int HB = 8 * NT, TPP = D / 4, AT_ONCE = JOIN_THREADS / TPP, PART = HB * (D + 2);
-  __shared__ float4 sums[AT_ONCE][TPP];
-  __shared__ float ls[AT_ONCE], tops[JOIN_THREADS / 32];
-  const int b = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int g = a.h / a.h_kv;
-  if (head >= g) return;
+__global__ void __launch_bounds__(JOIN_WARPS * 32) paged_join_kernel(const __grid_constant__ PagedAttn a) {
+  constexpr int HB = 8 * NT, PART = HB * (D + 2);
+  __shared__ float4 sums[JOIN_WARPS][D / 4];
+  __shared__ float ls[JOIN_WARPS];
+  const int b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   // its parts: the second of block b, the first of the blocks behind it up to the one where it ends
   int4 rec = make_int4(0, 0, 2, 0);
   if (b + lane < gridDim.x) rec = __ldcg(a.rec + b + lane);
   const int r = __shfl_sync(0xffffffffu, rec.x, 0), item = __shfl_sync(0xffffffffu, rec.y, 0);
   if (r < 0) return;
-  const int m = item / a.groups, hg = item - m * a.groups;
-  if (head >= min(HB, g - hg * HB)) return;
+  const int g = a.h / a.h_kv, m = item_m(item), hg = item_hg(item);
+  if (head >= g - hg * HB) return;
   int n = 1;
   for (int at = b;; at += 32) {
     if (at > b) rec.z = at + lane < gridDim.x ? __ldcg(&a.rec[at + lane].z) : 2;
@@ -426,33 +507,25 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const __grid_c
   }
   const float *const first = a.part + ((size_t)b * 2 + 1) * PART, *const others = a.part + (size_t)b * 2 * PART;   // (part i > 0)
   auto part = [&](int i) { return i == 0 ? first : others + (size_t)i * 2 * PART; };
-  // this thread's columns of its first parts, on their way while the scale is found
-  const int slot = tid / TPP, c4 = tid - slot * TPP;
   float4 o[JOIN_BATCH];
   float2 ml[JOIN_BATCH];
   auto fetch = [&](int i0) {
 #pragma unroll
     for (int u = 0; u < JOIN_BATCH; u++) {
-      const int i = i0 + u * AT_ONCE + slot;
+      const int i = i0 + u * JOIN_WARPS + warp;
       o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
       ml[u] = make_float2(-INFINITY, 0.f);
-      if (i < n && slot < AT_ONCE) {
-        o[u] = __ldcg(reinterpret_cast<const float4 *>(part(i) + head * D) + c4);
-        ml[u] = __ldcg(reinterpret_cast<const float2 *>(part(i) + HB * D) + head);
-      }
+      if (i < n) ml[u] = __ldcg(reinterpret_cast<const float2 *>(part(i) + HB * D) + head);
+      if (i < n && lane < D / 4) o[u] = __ldcg(reinterpret_cast<const float4 *>(part(i) + head * D) + lane);
     }
   };
   fetch(0);
   float top = -INFINITY;
-  for (int i = tid; i < n; i += JOIN_THREADS) top = fmaxf(top, __ldcg(part(i) + HB * D + head * 2));
+  for (int i = lane; i < n; i += 32) top = fmaxf(top, __ldcg(part(i) + HB * D + head * 2));
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-  if (lane == 0) tops[warp] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < JOIN_THREADS / 32; w++) top = fmaxf(top, tops[w]);
   const float ref = top == -INFINITY ? 0.f : top;
-  float l = 0.f;   // (of this thread's parts, in column 0's threads)
+  float l = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i0 = 0;;) {
 #pragma unroll
@@ -462,33 +535,30 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const __grid_c
       acc.z = fmaf(w, o[u].z, acc.z); acc.w = fmaf(w, o[u].w, acc.w);
       l = fmaf(w, ml[u].y, l);
     }
-    i0 += JOIN_BATCH * AT_ONCE;
+    i0 += JOIN_BATCH * JOIN_WARPS;
     if (i0 >= n) break;
     fetch(i0);
   }
-  if (slot < AT_ONCE) {
-    sums[slot][c4] = acc;
-    if (c4 == 0) ls[slot] = l;
-  }
+  if (lane < D / 4) sums[warp][lane] = acc;
+  if (lane == 0) ls[warp] = l;
   __syncthreads();
-  if (tid >= TPP) return;
-  l = 0.f;
-  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (warp > 0 || lane >= D / 4) return;
 #pragma unroll
-  for (int s = 0; s < AT_ONCE; s++) {
-    const float4 x = sums[s][tid];
+  for (int s = 1; s < JOIN_WARPS; s++) {
+    const float4 x = sums[s][lane];
     acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
     l += ls[s];
   }
   const int j = m * g + hg * HB + head;
   const float inv = 1.0f / l;
-  *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + r * a.out_req + j * a.out_head + tid * 4) =
+  *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + r * a.out_req + j * a.out_head + lane * 4) =
       make_uint2(Half2<T>::pack(acc.x * inv, acc.y * inv), Half2<T>::pack(acc.z * inv, acc.w * inv));
-  if (a.lse && tid == 0) a.lse[(size_t)r * a.h + j] = (top + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[(size_t)r * a.h + j] = (top + log2f(l)) * 0.6931471805599453f;
 }
 
 int heads_per_block(int h, int h_kv) { return h / h_kv > 8 ? 16 : 8; }
-int paged_blocks() { return sm_count_of_current_device() * PA_PER_SM; }
+int paged_blocks() { return sm_count_of_current_device() * 2; }
+static_assert(PaCfg<64, 1>::PER_SM == 2 && PaCfg<96, 1>::PER_SM == 2 && PaCfg<128, 1>::PER_SM == 2 && PaCfg<128, 2>::PER_SM == 2, "the grid");
 size_t part_floats(int h, int h_kv, int d) { return (size_t)heads_per_block(h, h_kv) * (d + 2); }
 
 template <typename T, int D, int NT>
@@ -497,10 +567,10 @@ cudaError_t launch(const PagedAttn &a, cudaStream_t st) {
   static PerDeviceFlag flag;
   cudaError_t e = allow_dynamic_smem(paged_attn_kernel<T, D, NT>, S::BYTES, flag);
   if (e != cudaSuccess) return e;
-  const int blocks = paged_blocks();
-  e = launch_kernel(paged_attn_kernel<T, D, NT>, dim3(blocks), dim3(PA_THREADS), S::BYTES, st, false, a);
+  const int blocks = paged_blocks(), g = a.h / a.h_kv;
+  e = launch_kernel(paged_attn_kernel<T, D, NT>, dim3(blocks), dim3(S::Cfg::WARPS * 32), S::BYTES, st, false, a);
   if (e != cudaSuccess) return e;
-  return launch_kernel(paged_join_kernel<T, D, NT>, dim3(blocks, 8 * NT), dim3(JOIN_THREADS), 0, st, true, a);
+  return launch_kernel(paged_join_kernel<T, D, NT>, dim3(blocks, g < 8 * NT ? g : 8 * NT), dim3(JOIN_WARPS * 32), 0, st, true, a);
 }
 
 template <typename T>
@@ -535,6 +605,12 @@ extern "C" int locret_paged_attention(const void *q, int64_t q_req, int64_t q_he
       window < 0 || sinks < 0 || !isfinite(scale))
     return LOCRET_ERR_INVALID;
   if ((q_req | q_head | out_req | out_head) & 7 || !aligned16p(q) || !aligned16p(out) || !aligned16p(workspace)) return LOCRET_ERR_INVALID;
+  const long double span = (long double)(pages->n_pages - 1) * pages->page_stride + (long double)(pages->page_size - 1) * pages->token_stride +
+                           (long double)(pages->n_kv_heads - 1) * pages->head_stride + pages->head_dim;
+  if (span / 8 >= 4294967296.0L) return LOCRET_ERR_INVALID;
+  // steps of the longest line there could be, a block's share of it (2^31 steps would take a block ten minutes)
+  const long double steps = ((long double)width * pages->page_size / 64 + 1) * n_req * n_q_heads;
+  if (steps / paged_blocks() >= 2147483648.0L) return LOCRET_ERR_INVALID;
   if (n_req == 0) return LOCRET_OK;
   if (!q || !table || !lens || !out || !workspace) return LOCRET_ERR_INVALID;
   int64_t need = 0;
@@ -546,7 +622,10 @@ extern "C" int locret_paged_attention(const void *q, int64_t q_req, int64_t q_he
   a.rec = static_cast<int4 *>(workspace);
   a.part = reinterpret_cast<float *>(a.rec + paged_blocks());
   a.table = table; a.lens = lens; a.table_stride = table_stride;
-  a.pages = page_view(*pages);
+  a.k = static_cast<const uint4 *>(pages->k); a.v = static_cast<const uint4 *>(pages->v);
+  a.page_stride = (uint32_t)(pages->page_stride / 8); a.head_stride = (uint32_t)(pages->head_stride / 8);
+  a.token_stride = (uint32_t)(pages->token_stride / 8);
+  a.n_pages = pages->n_pages; a.page_size = pages->page_size; a.by_size = FastDiv(pages->page_size);
   a.q_req = q_req; a.q_head = q_head; a.out_req = out_req; a.out_head = out_head;
   a.width = width; a.n_req = n_req; a.h = n_q_heads; a.h_kv = pages->n_kv_heads; a.groups = (g + hb - 1) / hb;
   a.window = window; a.sinks = sinks;

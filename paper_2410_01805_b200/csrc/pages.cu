@@ -191,6 +191,24 @@ __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_con
     const int count = (int)min(4ll, a.n_tok - t0);
     int64_t slot[4];
     int pos[4], p[4], off[4], r = t0 < n_rows ? owner(starts, a.n_req, (int)t0) : 0;
+    // four rows of one request (a prompt's), in two pages at most, or whatever they are
+    const int p0 = count == 4 && page >= 4 && t0 + 4 <= n_rows && starts[r + 1] >= (int)t0 + 4 && len[r] != REFUSED
+                       ? len[r] + ((int)t0 - starts[r]) : -1;
+    if (p0 >= 0) {
+      const int old = pages_of(len[r]), j0 = a.by_page.div(p0), o0 = p0 - j0 * page, j1 = o0 + 4 > page ? j0 + 1 : j0;
+      const int32_t *const row = a.table + r * a.table_stride;
+      const int32_t *const fresh = a.free_pages + (top - 1 - need0[r] + old);   // (page j of the request: fresh[-j])
+      const int a0 = *(j0 < old ? row + j0 : fresh - j0), a1 = *(j1 < old ? row + j1 : fresh - j1);
+      const bool ok0 = a0 >= 0 && a0 < a.capacity, ok1 = a1 >= 0 && a1 < a.capacity;
+      if (!ok0 || !ok1) report(a.status, LOCRET_ERR_INVALID);
+      const int64_t at0 = (int64_t)a0 * page + o0, at1 = (int64_t)a1 * page + o0 - page;
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        pos[u] = p0 + u;
+        p[u] = off[u] = 0;
+        slot[u] = o0 + u < page ? (ok0 ? at0 + u : -1) : (ok1 ? at1 + u : -1);
+      }
+    } else
 #pragma unroll
     for (int u = 0; u < 4; u++) {
       const int t = (int)t0 + u;
@@ -204,7 +222,7 @@ __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_con
           const int j = a.by_page.div(pos[u]), old = pages_of(n);
           off[u] = pos[u] - j * page;
           p[u] = j < old ? a.table[r * a.table_stride + j] : a.free_pages[top - 1 - (need0[r] + j - old)];
-          slot[u] = 0;
+          slot[u] = -2;   // (found, and to be made of p and off)
         } else {
           pos[u] = (int)max(0LL, min((long long)a.lens_in[r] + i, (long long)INT32_MAX));
         }
@@ -212,7 +230,7 @@ __global__ void __launch_bounds__(PS_THREADS) pages_step_kernel(const __grid_con
     }
 #pragma unroll
     for (int u = 0; u < 4; u++)
-      if (slot[u] == 0) {
+      if (slot[u] == -2) {
         if (p[u] >= 0 && p[u] < a.capacity) slot[u] = (int64_t)p[u] * page + off[u];
         else { slot[u] = -1; report(a.status, LOCRET_ERR_INVALID); }
       }

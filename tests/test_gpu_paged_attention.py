@@ -286,9 +286,10 @@ def test_refusals_need_no_gpu():
                 dict(ws=8)):
         assert call(**bad) == -1, bad
     assert call(size=need.value - 1) == -3
+    assert call(n=4096, width=2 ** 31 - 1, stride=2 ** 31 - 1, pages=C.byref(locret_pages(**{**pool, "page_size": 2 ** 20}))) == -1
     assert call(n=0, q=None, table=None, lens=None, out=None, ws=None) == 0
     for bad in (dict(k=None), dict(v=8), dict(n_pages=0), dict(page_size=0), dict(head_dim=80), dict(dtype=2), dict(dtype=-1),
-                dict(head_stride=-64), dict(token_stride=68)):
+                dict(head_stride=-64), dict(token_stride=68), dict(n_pages=2 ** 24 + 1), dict(head_stride=2 ** 35)):   # (64 GiB)
         assert call(pages=C.byref(locret_pages(**{**pool, **bad}))) == -1, bad
 
 
