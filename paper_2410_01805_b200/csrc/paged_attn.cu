@@ -74,7 +74,9 @@ struct PagedAttn {
 struct Visible {
   int n, shift, sinks;
   __device__ __forceinline__ int key(int i) const { return i < sinks ? i : i + shift; }
-  template <int STEP> __device__ __forceinline__ int steps() const { return n > 0 ? (n - 1) / STEP + 1 : 1; }   // (an empty request has one, to write zeros)
+  // (an empty request has one step, to write zeros)
+  template <int STEP> __device__ __forceinline__ int steps() const { return n > 0 ? (n - 1) / STEP + 1 : 1; }
+  template <int WARPS> __device__ __forceinline__ int steps(bool solo) const { return solo ? steps<16>() : steps<16 * WARPS>(); }
 };
 __device__ __forceinline__ int clamped_len(const PagedAttn &a, int r) {
   const int n = __ldg(a.lens + r);
@@ -92,19 +94,20 @@ __device__ __forceinline__ Visible visible_of(const PagedAttn &a, int len) {
 }
 
 // A place in the line: step `tile` of KV head m and block of heads hg of request r.
-template <int STEP>
+template <int WARPS>
 struct Cursor {
   int r, m, hg, tile, steps, next_len;   // next_len: of the request behind, on its way
   uint32_t head_at;                      // where head m begins in a page
   const int32_t *row;                    // the request's pages
   Visible v;
+  bool solo;
   __device__ __forceinline__ void enter(const PagedAttn &a, int request, int len) {
     r = request;
     m = hg = tile = 0;
     head_at = 0;
     row = a.table + r * a.table_stride;
     v = visible_of(a, len);
-    steps = v.template steps<STEP>();
+    steps = v.template steps<WARPS>(solo);
     next_len = clamped_len(a, min(r + 1, a.n_req - 1));
   }
   __device__ __forceinline__ void next(const PagedAttn &a) {
@@ -122,66 +125,123 @@ __device__ __forceinline__ int pack_item(int m, int hg) { return (int)((uint32_t
 __device__ __forceinline__ int item_m(int item) { return item & 0xffff; }
 __device__ __forceinline__ int item_hg(int item) { return (int)((uint32_t)item >> 16); }
 
-// The block's part [lo, hi) of the line, the request in which it begins, and how far into the request (in steps of all its
-// items).  With fewer steps than blocks the first blocks take one each, so that no block between two parts of an item is empty.
+// What a block - or, `solo`, a warp - does of the line: n steps from step `into` of request r (in steps of all its items).
+// Solo is for many short requests: a warp takes whole items, 16 keys a step, and the warps of a block need not meet, which costs
+// an item as much as about two steps.  A warp's share then ends with an item, so it is uneven by the longest of them; the
+// other way a block's share ends anywhere.  Taken where that makes the shorter time (413 requests of one or two tokens, eight
+// heads of 64: 33 us one way, 14.7 the other; 512 requests of 10 to 400 tokens, eight of 128: 115 and 110).
+struct Share {
+  int r, n;
+  long long into;
+  bool solo;
+};
 template <int WARPS>
-__device__ void find(const PagedAttn &a, int items, long long &lo, long long &hi, int &r_out, long long &into) {
-  constexpr int STEP = WARPS * 16, THREADS = WARPS * 32;
-  __shared__ long long warp_sums[WARPS], found_into;
-  __shared__ int found_r;
+__device__ Share find_share(const PagedAttn &a, int items) {
+  constexpr int THREADS = WARPS * 32;
+  __shared__ long long sums[2][WARPS], found_into[WARPS + 1];
+  __shared__ int longest[WARPS], found_r[WARPS + 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // every warp by itself for up to 32 requests, else the block
   const bool few = a.n_req <= 32;
   const int at = few ? lane : tid, per = few ? 1 : (a.n_req + THREADS - 1) / THREADS;
   const int r0 = min(a.n_req, at * per), r1 = min(a.n_req, r0 + per);
-  long long mine = 0;
+  long long mine_b = 0, mine_w = 0;   // steps of the thread's requests, for one item, by blocks and by warps
+  int most = 0;
   for (int r = r0; r < r1; r++) {
     const int raw = __ldg(a.lens + r), len = clamped_len(a, r);
     if (raw != len && blockIdx.x == 0) report(a.status, LOCRET_ERR_INVALID);
-    mine += visible_of(a, len).template steps<STEP>();
+    const Visible v = visible_of(a, len);
+    const int w = v.template steps<16>();
+    mine_b += v.template steps<16 * WARPS>();
+    mine_w += w;
+    most = max(most, w);
   }
-  long long x = mine;
+  long long upto_b = mine_b, upto_w = mine_w;   // with all before it
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    const long long y = __shfl_up_sync(0xffffffffu, upto_b, o), z = __shfl_up_sync(0xffffffffu, upto_w, o);
+    if (lane >= o) { upto_b += y; upto_w += z; }
   }
-  long long before = x - mine, total = __shfl_sync(0xffffffffu, x, 31);
+  most = __reduce_max_sync(0xffffffffu, most);
+  long long total_b = __shfl_sync(0xffffffffu, upto_b, 31), total_w = __shfl_sync(0xffffffffu, upto_w, 31);
   if (!few) {
-    if (lane == 31) warp_sums[warp] = x;
+    if (lane == 31) { sums[0][warp] = upto_b; sums[1][warp] = upto_w; longest[warp] = most; }
+    if (tid <= WARPS) { found_r[tid] = a.n_req; found_into[tid] = 0; }
     __syncthreads();
-    total = 0;
+    total_b = total_w = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; w++) {
-      if (w < warp) before += warp_sums[w];
-      total += warp_sums[w];
+      if (w < warp) { upto_b += sums[0][w]; upto_w += sums[1][w]; }
+      total_b += sums[0][w];
+      total_w += sums[1][w];
+      most = max(most, longest[w]);
     }
   }
-  total *= items;
-  const long long parts = min((long long)gridDim.x, total), part = min((long long)blockIdx.x, parts);
-  lo = total * part / parts;
-  hi = part < parts ? total * (part + 1) / parts : lo;
-  const bool here = lo < hi && before * items <= lo && lo < (before + mine) * items;
-  if (few) {
-    const int src = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
-    r_out = max(src, 0);
-    into = lo - __shfl_sync(0xffffffffu, before, r_out) * items;
-    return;
-  }
-  if (here) {
-    long long rest = lo - before * items;
-    int r = r0;
-    for (; r < r1; r++) {
-      const long long n = (long long)visible_of(a, clamped_len(a, r)).template steps<STEP>() * items;
-      if (rest < n) break;
+  total_b *= items;
+  total_w *= items;
+  const long long n_items = (long long)a.n_req * items, blocks = gridDim.x;
+  Share s;
+  s.solo = total_w + most * blocks * WARPS < (total_b + 2 * n_items) * WARPS;   // (shares, times the number of warps)
+  const long long mine = (s.solo ? mine_w : mine_b) * items, upto = (s.solo ? upto_w : upto_b) * items, total = s.solo ? total_w : total_b;
+  // With fewer steps than blocks the first blocks take one each, so that no block between two parts of an item is empty.
+  const long long parts = s.solo ? blocks * WARPS : min(blocks, total), first = (long long)blockIdx.x * (s.solo ? WARPS : 1);
+  const bool narrow = total * parts <= 0xffffffffll;   // (a division of 64 bits is a long way from the first request for a key)
+  auto cut = [&](long long part) {
+    part = min(part, parts);
+    return narrow ? (long long)((uint32_t)(total * part) / (uint32_t)parts) : total * part / parts;
+  };
+  // the request in which place p lies, if it is one of this thread's, and how far in
+  auto within = [&](long long p, long long &rest) {
+    rest = p - (upto - mine);
+    if (rest < 0 || rest >= mine) return -1;
+    for (int r = r0;; r++) {
+      const long long n = (long long)visible_of(a, clamped_len(a, r)).template steps<WARPS>(s.solo) * items;
+      if (rest < n) return r;
       rest -= n;
     }
-    found_r = r;
-    found_into = rest;
+  };
+  int r_lo = a.n_req, r_hi = a.n_req;   // (n_req: the line's end)
+  long long in_lo = 0, in_hi = 0;
+  const long long lo = cut(first + (s.solo ? warp : 0)), hi = cut(first + (s.solo ? warp : 0) + 1);
+  if (few) {
+    auto locate = [&](long long p, int &r, long long &in) {
+      long long rest;
+      const int mine_r = within(p, rest);
+      const unsigned who = __ballot_sync(0xffffffffu, mine_r >= 0);
+      if (who) {
+        r = __shfl_sync(0xffffffffu, mine_r, __ffs(who) - 1);
+        in = __shfl_sync(0xffffffffu, rest, __ffs(who) - 1);
+      }
+    };
+    locate(lo, r_lo, in_lo);
+    if (s.solo) locate(hi, r_hi, in_hi);
+  } else {
+    for (int k = 0; k < (s.solo ? WARPS + 1 : 1); k++) {
+      long long rest;
+      const int r = within(cut(first + k), rest);
+      if (r >= 0) { found_r[k] = r; found_into[k] = rest; }
+    }
+    __syncthreads();
+    const int k = s.solo ? warp : 0;
+    r_lo = found_r[k]; in_lo = found_into[k];
+    if (s.solo) { r_hi = found_r[k + 1]; in_hi = found_into[k + 1]; }
   }
-  __syncthreads();
-  r_out = found_r;
-  into = found_into;
+  long long n = hi - lo;
+  if (s.solo) {   // from the first item that begins at or behind a cut to the first at or behind the next cut
+    auto to_item = [&](int r, long long in) {
+      if (r >= a.n_req) return 0;
+      const int steps = visible_of(a, clamped_len(a, r)).template steps<16>(), tile = (int)(in % steps);
+      return tile ? steps - tile : 0;
+    };
+    const int skip = to_item(r_lo, in_lo);
+    n += to_item(r_hi, in_hi) - skip;
+    in_lo += skip;
+    if (r_lo < a.n_req && in_lo == (long long)visible_of(a, clamped_len(a, r_lo)).template steps<16>() * items) { r_lo++; in_lo = 0; }
+  }
+  s.r = r_lo;
+  s.into = in_lo;
+  s.n = (int)n;   // (the host refuses calls that could have more)
+  return s;
 }
 
 template <typename T, int D, int NT>
@@ -198,7 +258,7 @@ template <typename T, int D, int NT>
 __global__ void __launch_bounds__(PaCfg<D, NT>::WARPS * 32, PaCfg<D, NT>::PER_SM)
 paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   using S = PaSmem<T, D, NT>;
-  constexpr int PA_WARPS = PaCfg<D, NT>::WARPS, PA_STAGES = PaCfg<D, NT>::STAGES, PA_THREADS = PA_WARPS * 32, PA_STEP = PA_WARPS * 16;
+  constexpr int PA_WARPS = PaCfg<D, NT>::WARPS, PA_STAGES = PaCfg<D, NT>::STAGES, PA_THREADS = PA_WARPS * 32;
   constexpr int LD = S::LD, HB = S::HB, LF = S::LF, KD = D / 16;
   extern __shared__ __align__(16) unsigned char pa_smem[];
   __shared__ int4 info[PA_WARPS][PA_STAGES];
@@ -210,21 +270,21 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   using Cfg = PaCfg<D, NT>;
   pdl_launch_dependents();
 
-  long long lo, hi, into;
-  int r_first;
-  find<PA_WARPS>(a, items, lo, hi, r_first, into);
+  const Share share = find_share<PA_WARPS>(a, items);
+  const int n_steps = share.n;
+  const bool solo = share.solo;
   int4 rec = make_int4(-1, 0, 0, 0);
-  if (lo >= hi) {
+  if (n_steps == 0) {
     if (tid == 0) a.rec[blockIdx.x] = rec;
-    return;
+    return;   // (the whole block, or a warp that no other waits for)
   }
-  const int n_steps = (int)(hi - lo);   // (the host refuses calls that could have more)
 
-  Cursor<PA_STEP> load;
-  load.enter(a, r_first, clamped_len(a, r_first));
+  Cursor<PA_WARPS> load;
+  load.solo = solo;
+  load.enter(a, share.r, clamped_len(a, share.r));
   {
-    const int item = (int)(into / load.steps);
-    load.tile = (int)(into - (long long)item * load.steps);
+    const int item = share.into <= INT32_MAX ? (int)share.into / load.steps : (int)(share.into / load.steps);
+    load.tile = (int)(share.into - (long long)item * load.steps);
     load.m = item / a.groups;
     load.hg = item - load.m * a.groups;
     load.head_at = load.m * a.head_stride;
@@ -237,7 +297,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   int row_page = 0, row_j = 0, row_key = 0;
   bool row_there = false;
   auto look_up = [&]() {
-    const int i = load.tile * PA_STEP + warp * 16 + (lane & 15);
+    const int i = (solo ? load.tile : load.tile * PA_WARPS + warp) * 16 + (lane & 15);
     row_there = i < load.v.n;
     row_key = row_there ? load.v.key(i) : 0;
     row_j = a.by_size.div(row_key);
@@ -413,7 +473,45 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     __syncwarp();
 
     const bool ends = step.x >> 16 & 1;
-    if (ends || left == 1) {
+    if (ends && solo) {
+      // ---- the warp writes its item, half of the columns at a time through its own part of the buffer
+      const bool any = step.x >> 17 & 1;   // (a request of length 0: zeros)
+      const int m = item_m(step.z), hg = item_hg(step.z), gh = min(HB, g - hg * HB);
+      float *const mine = fo0 + warp * 8 * LF;
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) l_run[nt][e] += __shfl_xor_sync(0xffffffffu, l_run[nt][e], x);
+          if (g4 == 0) { wm[0][warp][nt * 8 + q4 * 2 + e] = m_run[nt][e]; wl[0][warp][nt * 8 + q4 * 2 + e] = l_run[nt][e]; }
+        }
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int side = 0; side < 2; side++) {
+#pragma unroll
+          for (int kk = 0; kk < KD / 2; kk++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+              mine[(q4 * 2 + (e & 1)) * LF + kk * 16 + g4 + (e >> 1) * 8] = o[nt][side * (KD / 2) + kk][e];
+          __syncwarp();
+#pragma unroll
+          for (int x = lane; x < 8 * (D / 8); x += 32) {
+            const int hh = x / (D / 8), c = (x - hh * (D / 8)) * 4, head = nt * 8 + hh, col = side * (D / 2) + c;
+            if (head >= gh) continue;
+            const float l = wl[0][warp][head], inv = any ? 1.0f / l : 0.f;
+            const float4 f = *reinterpret_cast<const float4 *>(mine + hh * LF + c);
+            const int j = m * g + hg * HB + head;
+            *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + step.y * a.out_req + j * a.out_head + col) =
+                make_uint2(Half2<T>::pack(f.x * inv, f.y * inv), Half2<T>::pack(f.z * inv, f.w * inv));
+            if (a.lse && col == 0)
+              a.lse[(size_t)step.y * a.h + j] = any ? (wm[0][warp][head] + log2f(l)) * 0.6931471805599453f : -INFINITY;
+          }
+          __syncwarp();
+        }
+      fresh = true;
+    } else if (ends || left == 1) {
       // ---- the warps meet: each leaves its sums as they are, and who adds them up weighs them by their scales
       const bool whole = ends && first_tile == 0, begins = first_tile == 0;
       const bool any = step.x >> 17 & 1;   // (a request of length 0: zeros)

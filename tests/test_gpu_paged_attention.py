@@ -96,6 +96,20 @@ def test_the_largest_batch():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("h,hk,d", [(32, 8, 128), (64, 32, 64), (32, 32, 96), (60, 5, 96), (48, 3, 128), (32, 2, 64)])
+@pytest.mark.parametrize("n,most", [(32, 16), (31, 40), (33, 1), (200, 33), (700, 100), (90, 260)])
+def test_many_short_requests(h, hk, d, n, most):
+    """Warps that take whole (request, KV head) items: up to 32 requests found by a warp, more by the block; lengths that fill
+    16 keys or not, empty requests first, last and between."""
+    rng = np.random.default_rng(n * 100 + most)
+    lens = rng.integers(0, most + 1, n)
+    lens[[0, n // 2, n - 1]] = 0
+    lens[[1, n // 3]] = most
+    check(make(lens.tolist(), h, hk, d, 16, torch.bfloat16, n + h), "bf16")
+    check(make(lens.tolist(), h, hk, d, 16, torch.float16, n + h), "fp16", window=max(1, most // 3), sinks=2)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("h,hk,d", HEADS[:4])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 3), (64, 0), (100, 4), (128, 64), (4096, 4), (17, 200), (2 ** 31 - 1, 9)])
 def test_windows_and_sinks(h, hk, d, window, sinks):
