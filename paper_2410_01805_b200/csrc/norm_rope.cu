@@ -211,10 +211,9 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// The warp's cosines and sines of one token, into its part of shared memory.
-__device__ __forceinline__ void fill_pairs(float2 *s, const NormRope &p, long long token) {
+// The warp's cosines and sines of a token at `position`, into its part of shared memory.
+__device__ __forceinline__ void fill_pairs(float2 *s, const NormRope &p, int position) {
   __syncwarp();
-  const int position = p.rot ? p.positions[token] : 0;
   for (int i = threadIdx.x & 31; i < p.rot / 2; i += 32) s[i] = cos_sin(p.turns[i], position, p.factor);
   __syncwarp();
 }
@@ -280,7 +279,7 @@ norm_rope_kernel(const __grid_constant__ NormRope p, int slices) {
       else if (lane == 0) report(p.status, LOCRET_ERR_INVALID);
     }
   }
-  fill_pairs(pairs[warp], p, tok);
+  fill_pairs(pairs[warp], p, p.rot ? p.positions[tok] : 0);
 
   int left = s1 - s0, kind = kind0, step = step0, stage = 0;
   while (left > 0) {   // (a kind)
@@ -410,11 +409,16 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
 #pragma unroll
   for (int i = 0; i < NRG_STAGES - 1; i++) ask();
   int stage = 0;
-  for (long long unit = (long long)b * NRG_WARPS + warp; unit < units; unit += stride) {
+  long long unit = (long long)b * NRG_WARPS + warp;
+  auto position_of = [&](long long unit) { return unit < units && p.rot ? p.positions[part.slices > 1 ? unit / part.slices : unit] : 0; };
+  int next_position = position_of(unit);
+  for (; unit < units; unit += stride) {
     long long tok;
     int s0, s1;
     steps_of(unit, tok, s0, s1);
-    fill_pairs(pairs[warp], p, tok);
+    const int position = next_position;
+    next_position = position_of(unit + stride);
+    fill_pairs(pairs[warp], p, position);
     const Turn<E> turn = turn_of<E, I, true>(pairs[warp], it, j, ones<E>());
     int head = s0 * R + row;
     T *to = dx + (tok * rows + head) * p.d + it.a;
