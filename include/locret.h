@@ -451,8 +451,8 @@ enum { LOCRET_BF16 = 0, LOCRET_FP16 = 1 };   /* dtype arguments */
 #define LOCRET_MAX_REQUESTS 4096             /* requests in one call */
 
 /* One layer's pool.  Column c of the key of token i of KV head m in page p: k + p * page_stride + m * head_stride +
- * i * token_stride + c, in elements; values likewise.  Pointers 16-byte aligned, strides multiples of 8 and >= 0.  locret_paged_attention takes
- * pools whose keys (and values) lie within 64 GiB. */
+ * i * token_stride + c, in elements; values likewise.  Pointers 16-byte aligned, strides multiples of 8 and >= 0.
+ * locret_paged_attention takes pools whose keys (and values) lie within 64 GiB. */
 typedef struct {
   void *k, *v;
   int32_t n_pages, page_size, n_kv_heads, head_dim;   /* page_size: tokens per page, any number >= 1 */
@@ -527,8 +527,9 @@ int locret_norm_rope(const locret_rope_args *args, void *stream);
  * are not looked at; q and k are the forward call's inputs (read only where there is a norm, may be NULL else).
  * d_q [n_tok x h x d], d_k [n_tok x h_kv x d]: type dtype, contiguous, 16-byte aligned, written whole; they may be the
  * buffers that held dL/dq_out and dL/dk_out if those are contiguous.  d_g_q, d_g_k: fp32 [d], given exactly where the norm is:
- * sums over tokens and heads, in an order that depends on the sizes alone.  workspace: device memory, 16-byte aligned, at least
- * the bytes that locret_norm_rope_grad_workspace reports (0 if there is no norm); contents need not be kept.
+ * sums over tokens and heads, in an order that depends on the sizes (and the device) alone.  workspace: device memory, 16-byte
+ * aligned, at least the bytes that locret_norm_rope_grad_workspace reports for the current device (NULL if there is no norm);
+ * contents need not be kept.
  */
 int locret_norm_rope_grad_workspace(int32_t head_dim, int64_t *bytes);
 int locret_norm_rope_grad(const locret_rope_args *args, void *d_q, void *d_k, float *d_g_q, float *d_g_k, void *workspace,
@@ -541,8 +542,8 @@ int locret_norm_rope_grad(const locret_rope_args *args, void *d_q, void *d_k, fl
  *     out[r][j] = sum_i softmax_i(scale * q[r][j] . k_i) v_i ,   KV head j / (h / h_kv)
  * A request of length 0 gets zeros.  Pages that hold no visible key are not read, and their table entries not looked at.
  * Several requests may name the same pages.
- * q, out: type of the pool, element (r, j, c) at r * *_req + j * *_head + c, 16-byte aligned, strides multiples of 8; lse: fp32
- * [n_req x h] or NULL, the logarithm of the sum of exp(scale * q . k) (-inf for length 0).  table, lens: device int32 as in
+ * q, out: type of the pool, element (r, j, c) at r * *_req + j * *_head + c, 16-byte aligned, strides multiples of 8; out
+ * overlaps nothing that is read.  lse: fp32 [n_req x h] or NULL, the logarithm of the sum of exp(scale * q . k) (-inf for length 0).  table, lens: device int32 as in
  * locret_pages_step; a length outside [0, width * page_size] is taken as the nearer end, a key in a page that does not exist
  * as absent, both reported.  scale: any finite number (1 / sqrt(d) in Eq. 1).  head_dim 64, 96 or 128; h a multiple of h_kv;
  * 0 <= n_req <= LOCRET_MAX_REQUESTS.

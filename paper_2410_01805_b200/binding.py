@@ -239,9 +239,13 @@ class LocretLayer:
                     S=S, T=T, seen=seen.value)
 
     def export_pages(self, pages, table_row: torch.Tensor, status: torch.Tensor | None = None):
-        """The retained units into pages (a Pages): unit i into token i % page_size of page table_row[i // page_size]."""
+        """The retained units into pages (a Pages): unit i into token i % page_size of page table_row[i // page_size].
+        Asynchronous on the layer's stream."""
         if not (table_row.is_cuda and table_row.dtype == torch.int32 and table_row.dim() == 1 and table_row.is_contiguous()):
             raise ValueError("table_row must be a contiguous CUDA int32 vector")
+        if pages.k.device != table_row.device or table_row.get_device() != torch.cuda.current_device() or (
+                status is not None and (status.device != table_row.device or status.dtype != torch.int32)):
+            raise ValueError("pages, table_row and status (int32) must lie on the current device")
         _check(lib.locret_export_pages(self._h, pages.address, table_row.data_ptr(), table_row.numel(),
                                        status.data_ptr() if status is not None else None), "locret_export_pages")
 

@@ -48,7 +48,7 @@ def module_command():
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *("-I" + p for p in include), MODULE_SRC,
             "-o", MODULE, "-L" + HERE, "-l:liblocret.so", "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch",
-            "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
+            "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -21,8 +21,10 @@
 namespace locret {
 namespace {
 
-// Warps of a block, stages of a warp's ring, blocks of an SM.  What the loop waits for is its own chain of instructions, so more
-// warps do more than more stages, as far as shared memory and registers go.
+// Warps of a block, stages of a warp's ring, blocks of an SM, and whether there are two buffers in which the warps meet.  What the
+// loop waits for is its own chain of instructions, so more warps do more than more stages, as far as shared memory goes (four
+// warps with three stages each, then these: two KV heads of 64, 1.03 GB: 192, 171 us; 32 of 96, a window, 1.05 GB: 181, 174; eight
+// of 128, one request, 4.1 GB: 655, 630).  With sixteen heads a block, five warps of two stages take 122 us for 109.
 template <int D, int NT> struct PaCfg { static constexpr int WARPS = 4, STAGES = 3, PER_SM = 2; static constexpr bool TWO = false; };
 template <> struct PaCfg<128, 1> { static constexpr int WARPS = 5, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
 template <> struct PaCfg<96, 1> { static constexpr int WARPS = 5, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };

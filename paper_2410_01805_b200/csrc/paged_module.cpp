@@ -1,6 +1,6 @@
 // Python entry points of the calls on pages.  A step of a served batch calls each of them once per decoder layer, for kernels of a
 // few microseconds: through ctypes and Python's own checks a call cost 23 to 37 us of the host's time, more than the kernels of a
-// small batch take, so these calls are checked, allocated for and launched here (6 to 11 us, one or two launches among them).
+// small batch take, so these calls are checked, allocated for and launched here (5 to 9 us, one or two launches among them).
 //
 // Everything is as in the C entry points (include/locret.h), on torch's current stream; what can be seen of the tensors is checked
 // and refused with ValueError, what the library returns is raised as LocretError.
@@ -9,6 +9,7 @@
 #include <structmember.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -108,7 +109,7 @@ struct Where {
   }
 };
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Where &w) {
-  return at::empty(shape, at::TensorOptions().dtype(type).device(w.device));
+  return at::detail::empty_cuda(shape, type, w.device, c10::nullopt);   // (at::empty without the dispatcher)
 }
 
 // words (lengths, tables, positions ...): a type, a number of dimensions, the last one contiguous
@@ -133,6 +134,13 @@ const at::Tensor &heads(PyObject *o, const char *what, at::ScalarType type, cons
   if (t.dim() != 3 || t.scalar_type() != type || t.device() != w.device || (t.size(2) > 1 && t.stride(2) != 1))
     refuse(std::string(what) + " must have three dimensions (tokens, heads, d), type " + c10::toString(type) + ", lie on " +
            w.device.str() + " and be contiguous in the last dimension");
+  return t;
+}
+// where a call writes: no two elements in one place
+const at::Tensor &written(PyObject *o, const char *what, at::ScalarType type, const Where &w) {
+  const at::Tensor &t = heads(o, what, type, w);
+  for (int i = 0; i < 2; i++)
+    if (t.size(i) > 1 && t.stride(i) == 0) refuse(std::string(what) + " is an expanded tensor");
   return t;
 }
 void same_shape(const at::Tensor &a, const at::Tensor &b, const char *what) {
@@ -311,8 +319,8 @@ PyObject *norm_rope(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *k
     input(r.q, r.q_token, r.q_head, q);
     input(r.k, r.k_token, r.k_head, k);
     at::Tensor q_out, k_out;
-    if (a.v[9]) q_out = heads(a.v[9], "q_out", type, w);
-    if (a.v[10]) k_out = heads(a.v[10], "k_out", type, w);
+    if (a.v[9]) q_out = written(a.v[9], "q_out", type, w);
+    if (a.v[10]) k_out = written(a.v[10], "k_out", type, w);
     if (a.v[12]) {
       const at::Tensor &v = heads(a.v[11], "v", type, w), *slots;
       same_shape(v, k, "v and k");
@@ -402,7 +410,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObj
     const int32_t h = (int32_t)q.size(1);
     at::Tensor out, lse;
     if (a.v[7]) {
-      out = heads(a.v[7], "out", q.scalar_type(), w);
+      out = written(a.v[7], "out", q.scalar_type(), w);
       same_shape(out, q, "out and q");
     } else {
       out = empty(q.sizes(), q.scalar_type(), w);

@@ -318,7 +318,7 @@ def test_the_binding_refuses_what_it_can_see():
     P.norm_rope(**good)
     for bad in (dict(q=q.cpu()), dict(k=k.half()), dict(k=k[:3]), dict(positions=pos.long()), dict(positions=pos[:3]),
                 dict(turns=turns.float()), dict(g_q=gq.float()), dict(g_q=gq[:32]), dict(v=v), dict(pages=pages), dict(q=q[0]),
-                dict(q=q.transpose(1, 2)), dict(q_out=torch.empty_like(q)[:2]), dict(pages=pages, v=v, slots=slots.int()),
+                dict(q=q.transpose(1, 2)), dict(q_out=torch.empty_like(q)[:2]), dict(q_out=torch.empty_like(q)[:1].expand(4, -1, -1)), dict(k_out=q), dict(pages=pages, v=v, slots=slots.int()),
                 dict(pages=pages, v=v[:, :1], slots=slots), dict(status=torch.zeros(1, device="cuda"))):
         with pytest.raises(ValueError):
             P.norm_rope(**{**good, **bad})

@@ -315,7 +315,7 @@ def test_the_binding_refuses_what_it_can_see():
     P.paged_attention(**good)
     for bad in (dict(q=q.cpu()), dict(q=q.half()), dict(q=q[:, :, :32]), dict(q=q[0]), dict(table=table.long()), dict(table=table[:1]),
                 dict(lens=lens[:1]), dict(lens=lens.long()), dict(lens=lens.cpu()), dict(out=torch.empty_like(q)[:1]),
-                dict(out=torch.empty_like(q).half()), dict(status=lens.long())):
+                dict(out=torch.empty_like(q).half()), dict(out=torch.empty_like(q)[:1].expand(2, -1, -1)), dict(status=lens.long())):
         with pytest.raises(ValueError):
             P.paged_attention(**{**good, **bad})
     for bad in (dict(window=-1), dict(sinks=-2), dict(scale=math.inf), dict(q=q[:, :3])):

@@ -207,6 +207,9 @@ def test_a_layers_units_into_pages(name, page):
     status.zero_()
     layer.export_pages(pages, row, status)
     assert status.item() == -1
+    for bad in (dict(table_row=row.cpu()), dict(table_row=row.long()), dict(table_row=row[::2]), dict(status=status.cpu())):
+        with pytest.raises(ValueError):
+            layer.export_pages(**{**dict(pages=pages, table_row=row, status=status), **bad})
     with pytest.raises(P.LocretError):   # no room
         layer.export_pages(pages, row[:3], status)
     with pytest.raises(P.LocretError):   # another head size
