@@ -110,6 +110,25 @@ def test_many_short_requests(h, hk, d, n, most):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("h,hk,d", [(32, 8, 128), (32, 32, 96), (8, 2, 64), (40, 4, 128)])
+@pytest.mark.parametrize("n,most", [(1, 100), (40, 150), (40, 400), (75, 300), (20, 640), (3, 2000)])
+def test_items_that_are_not_divided(h, hk, d, n, most):
+    """Tables that have room for a few steps only: blocks take whole items where there are enough, or hardly a step."""
+    rng = np.random.default_rng(n + most)
+    lens = rng.integers(most // 2, most + 1, n)
+    lens[0] = most
+    case = make(lens.tolist(), h, hk, d, 16, torch.bfloat16, n + h)
+    out, lse = check(case, "bf16")
+    # the same requests under a table with room for long ones: divided, and the same up to the order of the sums
+    import paper_2410_01805_b200 as P
+    q, k, v, table, n_ = case
+    wide = torch.full((n, 5000), -1, dtype=I32, device="cuda")
+    wide[:, : table.shape[1]] = table
+    far = P.paged_attention(q, P.Pages(k, v), wide, n_)
+    assert (far.double() - out.double()).abs().max() <= 2.0 ** -7 * out.double().abs().max()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("h,hk,d", HEADS[:4])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 3), (64, 0), (100, 4), (128, 64), (4096, 4), (17, 200), (2 ** 31 - 1, 9)])
 def test_windows_and_sinks(h, hk, d, window, sinks):
