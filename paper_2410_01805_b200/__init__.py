@@ -1,7 +1,7 @@
 """B200-native chunked-prefill step with retaining-head eviction (Locret).
 
-The package is a thin ctypes binding over ``liblocret.so`` (hand-written CUDA for
-sm_100a).  Every step of the path runs in the library's kernels; Python only
+The package is a thin binding over ``liblocret.so`` (hand-written CUDA for sm_100a): ctypes, and the
+compiled module ``_paged`` for the calls on pages, which a served batch makes many times a step.  Every step of the path runs in the library's kernels; Python only
 marshals pointers.  There is no CPU fallback: importing the binding without the
 built library raises.
 """
