@@ -585,8 +585,9 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
 
 // Block (b, head) joins that head of the item that begins in block b's part of the line and ends in another's.  A chain of
 // latencies (records, then parts): a warp's lanes take four columns each, and JOIN_WARPS * JOIN_BATCH parts are requested before
-// one is used (one request of 6000 tokens, 38 parts an item: 23 us with a warp per head and a part after the other).
-constexpr int JOIN_WARPS = 4, JOIN_BATCH = 10;
+// one is used (one request of 6000 tokens, 38 parts an item: 23 us with a warp per head and a part after the other, 4.8 now).  Most
+// blocks find nothing to join and end: small ones, so that all of them fit at once (four warps: 61 requests 1.2 us longer).
+constexpr int JOIN_WARPS = 2, JOIN_BATCH = 10;
 
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) paged_join_kernel(const __grid_constant__ PagedAttn a) {

@@ -40,25 +40,43 @@ void check(int code, const char *what) {
   throw Raised();
 }
 
+// A function's argument names, as the interned strings that its callers' keywords are (compared by address first: by letters
+// alone, ten keywords took longer than the checks).
+template <int N>
+struct Names {
+  PyObject *interned[N];
+  explicit Names(const char *const (&names)[N]) {
+    for (int i = 0; i < N; i++) {
+      interned[i] = PyUnicode_InternFromString(names[i]);   // (kept for the life of the process)
+      if (!interned[i]) throw Raised();
+    }
+  }
+  int find(PyObject *name) const {
+    for (int i = 0; i < N; i++)
+      if (interned[i] == name) return i;
+    for (int i = 0; i < N; i++)
+      if (PyUnicode_Compare(interned[i], name) == 0) return i;
+    return -1;
+  }
+};
+
 // Positional and keyword arguments, by name; the first `required` have to be there.  None counts as absent.
 template <int N>
 struct Args {
   PyObject *v[N] = {};
-  Args(const char *func, const char *const (&names)[N], int required, PyObject *const *args, Py_ssize_t n, PyObject *kwnames) {
+  Args(const char *func, const Names<N> &names, int required, PyObject *const *args, Py_ssize_t n, PyObject *kwnames) {
     if (n > N) fail(func, "takes at most " + std::to_string(N) + " arguments");
     for (Py_ssize_t i = 0; i < n; i++) v[i] = args[i];
     const Py_ssize_t n_kw = kwnames ? PyTuple_GET_SIZE(kwnames) : 0;
     for (Py_ssize_t k = 0; k < n_kw; k++) {
       PyObject *name = PyTuple_GET_ITEM(kwnames, k);
-      int at = -1;
-      for (int i = 0; i < N && at < 0; i++)
-        if (PyUnicode_CompareWithASCIIString(name, names[i]) == 0) at = i;
+      const int at = names.find(name);
       if (at < 0 || v[at]) fail(func, std::string(at < 0 ? "got an unexpected argument '" : "got two values for '") + PyUnicode_AsUTF8(name) + "'");
       v[at] = args[n + k];
     }
     for (int i = 0; i < N; i++) {
       if (v[i] == Py_None) v[i] = nullptr;
-      if (!v[i] && i < required) fail(func, std::string("needs '") + names[i] + "'");
+      if (!v[i] && i < required) fail(func, std::string("needs '") + PyUnicode_AsUTF8(names.interned[i]) + "'");
     }
   }
   [[noreturn]] static void fail(const char *func, const std::string &why) {
@@ -233,7 +251,7 @@ PyStructSequence_Desc step_desc = {"paper_2410_01805_b200.PagesStep", "What a st
 
 PyObject *pages_step(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *kwnames) {
   return guarded([&]() -> PyObject * {
-    static const char *const names[] = {"table", "lens", "new_lens", "free_pages", "n_free", "page_size", "n_tok", "lens_out", "n_free_out", "status"};
+    static const Names<10> names({"table", "lens", "new_lens", "free_pages", "n_free", "page_size", "n_tok", "lens_out", "n_free_out", "status"});
     const Args<10> a("pages_step", names, 7, argv, n, kwnames);
     const at::Tensor &table = tensor(a.v[0], "table");
     const Where w(table, "table");
@@ -307,7 +325,7 @@ void output(void *&p, int64_t &token, int64_t &head, const at::Tensor &t) { p = 
 
 PyObject *norm_rope(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *kwnames) {
   return guarded([&]() -> PyObject * {
-    static const char *const names[] = {"q", "k", "positions", "turns", "factor", "interleaved", "g_q", "g_k", "eps", "q_out", "k_out", "v", "pages", "slots", "status"};
+    static const Names<15> names({"q", "k", "positions", "turns", "factor", "interleaved", "g_q", "g_k", "eps", "q_out", "k_out", "v", "pages", "slots", "status"});
     const Args<15> a("norm_rope", names, 4, argv, n, kwnames);
     const at::Tensor &q0 = tensor(a.v[0], "q");
     const Where w(q0, "q");
@@ -350,7 +368,7 @@ PyObject *norm_rope(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *k
 
 PyObject *norm_rope_grad(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *kwnames) {
   return guarded([&]() -> PyObject * {
-    static const char *const names[] = {"dq_out", "dk_out", "q", "k", "positions", "turns", "factor", "interleaved", "g_q", "g_k", "eps"};
+    static const Names<11> names({"dq_out", "dk_out", "q", "k", "positions", "turns", "factor", "interleaved", "g_q", "g_k", "eps"});
     const Args<11> a("norm_rope_grad", names, 2, argv, n, kwnames);
     const at::Tensor &dq0 = tensor(a.v[0], "dq_out");
     const Where w(dq0, "dq_out");
@@ -397,7 +415,7 @@ PyObject *norm_rope_grad(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObje
 // ---------------------------------------------------------------- paged_attention
 PyObject *paged_attention(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *kwnames) {
   return guarded([&]() -> PyObject * {
-    static const char *const names[] = {"q", "pages", "table", "lens", "scale", "window", "sinks", "out", "with_lse", "status"};
+    static const Names<10> names({"q", "pages", "table", "lens", "scale", "window", "sinks", "out", "with_lse", "status"});
     const Args<10> a("paged_attention", names, 4, argv, n, kwnames);
     const at::Tensor &q0 = tensor(a.v[0], "q");
     const Where w(q0, "q");
