@@ -1,6 +1,6 @@
 // Python entry points of the calls on pages.  A step of a served batch calls each of them once per decoder layer, for kernels of a
 // few microseconds: through ctypes and Python's own checks a call cost 23 to 37 us of the host's time, more than the kernels of a
-// small batch take, so these calls are checked, allocated for and launched here (5 to 9 us, one or two launches among them).
+// small batch take, so these calls are checked, allocated for and launched here (4 to 9 us, one or two launches among them).
 //
 // Everything is as in the C entry points (include/locret.h), on torch's current stream; what can be seen of the tensors is checked
 // and refused with ValueError, what the library returns is raised as LocretError.
