@@ -474,6 +474,7 @@ typedef struct {
  * A request is refused - table, list and length as they were, its rows get slot -1 - if its length is outside
  * [0, width * page_size] (LOCRET_ERR_INVALID), or if its tokens have no room in width pages, in n_tok rows or in what is left
  * of the list after the requests before it, refused ones counted (LOCRET_ERR_CAPACITY).
+ * The list keeps no count of owners: a page that several requests name may be given back by one of them only, the last.
  * 0 <= n_req <= LOCRET_MAX_REQUESTS, 0 <= n_tok, 1 <= page_size, width, capacity.  The arrays must not overlap otherwise.
  */
 int locret_pages_step(int32_t *table, int64_t table_stride, int32_t width, const int32_t *lens_in, int32_t *lens_out,

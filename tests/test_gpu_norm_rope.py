@@ -92,6 +92,12 @@ def test_forward(n, h, hk, d, rot, dtype, interleaved, norm):
     ref[slots[there] // page, slots[there] % page, 0] = ko[there]
     ref[slots[there] // page, slots[there] % page, 1] = v[there]
     assert torch.equal(pool, ref)
+    # into parts of larger buffers, the rotated keys into one of them as well as into the pages
+    big = torch.full((n + 1, h + hk + 2, d), 5.0, dtype=dt, device="cuda")
+    pool.fill_(7.0)
+    qo3, ko3 = P.norm_rope(q, k, pos, turns, q_out=big[:n, 1:1 + h], k_out=big[:n, 1 + h:1 + h + hk], v=v, pages=pages, slots=slots, **kw)
+    assert torch.equal(qo3, qo) and torch.equal(ko3, ko) and torch.equal(pool, ref)
+    assert (big[n] == 5).all() and (big[:, 0] == 5).all() and (big[:, -1] == 5).all()
     # in place
     P.norm_rope(q, k, pos, turns, q_out=q, k_out=k, **kw)
     assert torch.equal(q, qo) and torch.equal(k, ko)
