@@ -440,12 +440,13 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
 #pragma unroll
         for (int e = 0; e < E / 2; e++) w.v[e] = mul_f32x2(y.v[e], gain.v[e]);
         const float ss = group_sum<G>(dot2(x, x)), dot = group_sum<G>(dot2(w, x));
-        const float rstd = rsqrtf(fmaf(ss, p.inv_d, p.eps)), mean = dot * rstd * p.inv_d;
+        // (a row that is not there: zeros, and without an epsilon their factor would be infinite)
+        const float rstd = head < rows ? rsqrtf(fmaf(ss, p.inv_d, p.eps)) : 0.f, mean = dot * rstd * p.inv_d;
         const uint64_t r2 = both(rstd), m2 = both(-mean * rstd);
 #pragma unroll
         for (int e = 0; e < E / 2; e++) {
           const uint64_t unit2 = mul_f32x2(x.v[e], r2);
-          dg.v[e] = fma_f32x2(y.v[e], unit2, dg.v[e]);   // (rows that are not there: zeros)
+          dg.v[e] = fma_f32x2(y.v[e], unit2, dg.v[e]);
           y.v[e] = fma_f32x2(unit2, m2, mul_f32x2(w.v[e], r2));
         }
       }
