@@ -12,6 +12,7 @@
 //    is found and the sums are rescaled): most steps need one vote in place of the reductions.
 //  * The warps of a block meet at the end of a (request, KV head); where the line was cut inside one, the blocks leave partial
 //    results that a second kernel joins, in the order of the blocks.
+#include <float.h>
 #include <math.h>
 
 #include "../../include/locret.h"
@@ -316,8 +317,8 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     const uint32_t mask = __ballot_sync(0xffffffffu, row_there) & 0xffffu;
     const uint32_t at = row_there ? row_page * a.page_stride + (row_key - row_j * a.page_size) * a.token_stride + load.head_at : 0;
     // what the step is, for the warp that will work on it: keys that exist | last of its item, request, item, step of the item
-    if (lane == 0) info[warp][stage] = make_int4((int)mask | (load.tile + 1 == load.steps ? 1 << 16 : 0) | (load.v.n > 0 ? 1 << 17 : 0),
-                                                 load.r, pack_item(load.m, load.hg), load.tile);
+    if (lane == 0) info[warp][stage] = make_int4((int)mask | (load.tile + 1 == load.steps ? 1 << 16 : 0), load.r,
+                                                 pack_item(load.m, load.hg), load.tile);
     T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
 #pragma unroll
     for (int x = 0; x < COPIES; x++) {
@@ -358,6 +359,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   int set = 0;
   float o[NT][KD][4], m_run[NT][2], l_run[NT][2];
   float m_ref[NT][2], m_most[NT][2];   // the scale as it is subtracted (0 for -inf), and what a score may not exceed
+  uint32_t seen = 0;                   // keys of the item that exist, over its steps
   bool fresh = true;                   // the state belongs to no item yet
   int first_tile = 0, stage = 0;
   for (int left = n_steps; left > 0; left--) {
@@ -366,6 +368,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     const int4 step = info[warp][stage];
     if (fresh) {
       fresh = false;
+      seen = 0;
       first_tile = step.w;
       const int m = item_m(step.z), hg = item_hg(step.z);
       // the item's queries, requested when the last one began, and the next one's
@@ -399,6 +402,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
 
     const T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
     const uint32_t mask = step.x & 0xffff;
+    seen |= mask;
     if (mask) {
       float s[NT][4] = {};
 #pragma unroll
@@ -478,9 +482,16 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     __syncwarp();
 
     const bool ends = step.x >> 16 & 1;
+    // A scale of -inf says that there was no key (the output is 0).  Keys whose scores are all -inf, which give NaN, have the lowest
+    // finite one: beside others it makes a weight of 0 as well.
+    if (seen && (ends || left == 1)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) m_run[nt][e] = fmaxf(m_run[nt][e], -FLT_MAX);
+    }
     if (ends && solo) {
       // ---- the warp writes its item, half of the columns at a time through its own part of the buffer
-      const bool any = step.x >> 17 & 1;   // (a request of length 0: zeros)
       const int m = item_m(step.z), hg = item_hg(step.z), gh = min(HB, g - hg * HB);
       float *const mine = fo0 + warp * 8 * LF;
 #pragma unroll
@@ -505,13 +516,13 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
           for (int x = lane; x < 8 * (D / 8); x += 32) {
             const int hh = x / (D / 8), c = (x - hh * (D / 8)) * 4, head = nt * 8 + hh, col = side * (D / 2) + c;
             if (head >= gh) continue;
-            const float l = wl[0][warp][head], inv = any ? 1.0f / l : 0.f;
+            const float top = wm[0][warp][head], l = wl[0][warp][head], inv = top == -INFINITY ? 0.f : 1.0f / l;
             const float4 f = *reinterpret_cast<const float4 *>(mine + hh * LF + c);
             const int j = m * g + hg * HB + head;
             *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + step.y * a.out_req + j * a.out_head + col) =
                 make_uint2(Half2<T>::pack(f.x * inv, f.y * inv), Half2<T>::pack(f.z * inv, f.w * inv));
             if (a.lse && col == 0)
-              a.lse[(size_t)step.y * a.h + j] = any ? (wm[0][warp][head] + log2f(l)) * 0.6931471805599453f : -INFINITY;
+              a.lse[(size_t)step.y * a.h + j] = top == -INFINITY ? top : (top + log2f(l)) * 0.6931471805599453f;
           }
           __syncwarp();
         }
@@ -519,7 +530,6 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     } else if (ends || left == 1) {
       // ---- the warps meet: each leaves its sums as they are, and who adds them up weighs them by their scales
       const bool whole = ends && first_tile == 0, begins = first_tile == 0;
-      const bool any = step.x >> 17 & 1;   // (a request of length 0: zeros)
       const int m = item_m(step.z), hg = item_hg(step.z), gh = min(HB, g - hg * HB);
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
@@ -560,10 +570,10 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
             }
             const int j = m * g + hg * HB + head;
             if (whole) {
-              const float inv = any ? 1.0f / l : 0.f;
+              const float inv = top == -INFINITY ? 0.f : 1.0f / l;
               *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + step.y * a.out_req + j * a.out_head + col) =
                   make_uint2(Half2<T>::pack(sum.x * inv, sum.y * inv), Half2<T>::pack(sum.z * inv, sum.w * inv));
-              if (a.lse && col == 0) a.lse[(size_t)step.y * a.h + j] = any ? (top + log2f(l)) * 0.6931471805599453f : -INFINITY;
+              if (a.lse && col == 0) a.lse[(size_t)step.y * a.h + j] = top == -INFINITY ? top : (top + log2f(l)) * 0.6931471805599453f;
             } else {
               *reinterpret_cast<float4 *>(part + head * D + col) = sum;
               if (col == 0) *reinterpret_cast<float2 *>(part + HB * D + head * 2) = make_float2(top, l);
@@ -654,10 +664,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) paged_join_kernel(const __gri
     l += ls[s];
   }
   const int j = m * g + hg * HB + head;
-  const float inv = 1.0f / l;
+  const float inv = top == -INFINITY ? 0.f : 1.0f / l;   // (no part has seen a key)
   *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + r * a.out_req + j * a.out_head + lane * 4) =
       make_uint2(Half2<T>::pack(acc.x * inv, acc.y * inv), Half2<T>::pack(acc.z * inv, acc.w * inv));
-  if (a.lse && lane == 0) a.lse[(size_t)r * a.h + j] = (top + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[(size_t)r * a.h + j] = top == -INFINITY ? top : (top + log2f(l)) * 0.6931471805599453f;
 }
 
 int heads_per_block(int h, int h_kv) { return h / h_kv > 8 ? 16 : 8; }

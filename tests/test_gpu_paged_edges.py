@@ -1,12 +1,14 @@
 """Calls on pages at the edges of what they accept."""
 
+import math
+
 import numpy as np
 import pytest
 import torch
 
 import paged_util as U
 from test_gpu_norm_rope import close, expected, f64, tensors, turns_of
-from test_gpu_paged_attention import TYPES
+from test_gpu_paged_attention import I32, TYPES, check, make
 
 
 @pytest.mark.gpu
@@ -34,3 +36,60 @@ def test_gradients_without_an_epsilon(n, h, hk, d, rot, dtype, interleaved):
         # fp32 roundings), and, whatever the order, no more than n * heads + 64 additions of 2^-24 of the sum of magnitudes
         terms = (mag * np.abs(xx * r)).sum((0, 1))
         assert (np.abs(f64(dg) - want_g) <= terms * (2.0 ** -19 + (n * x.shape[1] + 64) * 2.0 ** -24)).all()
+
+
+# (requests, their lengths, room in the table): items of warps, of blocks, divided and joined
+PATHS = [("warps", [40, 3, 17, 1] * 80, 40), ("blocks", [100, 64, 90], 100), ("joined", [6000, 300, 9000], 9000),
+         ("joined", [20, 3], 5000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("path,lens,most", PATHS)
+@pytest.mark.parametrize("h,hk,d,dtype", [(8, 2, 64, "bf16"), (32, 2, 128, "fp16"), (6, 3, 96, "bf16")])
+def test_requests_none_of_whose_pages_exist(path, lens, most, h, hk, d, dtype):
+    """Keys in pages that do not exist are absent; a request that has no others gets what an empty one gets, and is reported."""
+    import paper_2410_01805_b200 as P
+    q, k, v, table, n = make(lens, h, hk, d, 16, TYPES[dtype][0], len(lens))
+    wide = torch.full((len(lens), -(-most // 16)), -1, dtype=I32, device="cuda")
+    wide[:, : table.shape[1]] = table
+    want, want_lse = check((q, k, v, wide, n), dtype)
+    gone = [0, len(lens) - 1]
+    for bad in (-1, k.shape[0], 2 ** 31 - 1):
+        t = wide.clone()
+        t[gone] = bad
+        status = torch.zeros(1, dtype=I32, device="cuda")
+        out, lse = P.paged_attention(q, P.Pages(k, v), t, n, with_lse=True, status=status)
+        assert (out[gone] == 0).all() and torch.isneginf(lse[gone]).all() and status.item() == -1
+        rest = [r for r in range(len(lens)) if r not in gone]
+        assert torch.equal(out[rest], want[rest]) and torch.equal(lse[rest], want_lse[rest])
+    # a length beyond the table, whose window lies where there are no pages; and with first tokens, which there are
+    far = torch.full((len(lens), wide.shape[1] + 40), -1, dtype=I32, device="cuda")
+    far[:, : table.shape[1]] = table
+    n[gone[0]] = 2 ** 31 - 1
+    status = torch.zeros(1, dtype=I32, device="cuda")
+    out, lse = P.paged_attention(q, P.Pages(k, v), far, n, window=100, with_lse=True, status=status)
+    assert (out[gone[0]] == 0).all() and torch.isneginf(lse[gone[0]]).all() and status.item() == -1
+    assert torch.isfinite(out).all()
+    out, lse = P.paged_attention(q, P.Pages(k, v), far, n, window=100, sinks=1, with_lse=True)
+    first = v[table[gone[0], 0].long(), :, 0].repeat_interleave(h // hk, 0)   # (one key: its value is the answer)
+    assert torch.equal(out[gone[0]], first)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("path,lens,most", PATHS)
+def test_scores_that_are_all_minus_infinity_are_not_absent(path, lens, most):
+    """softmax over nothing but -inf is NaN, wherever the keys are; beside a finite one they weigh nothing."""
+    import paper_2410_01805_b200 as P
+    q, k, v, table, n = make(lens, 4, 1, 64, 16, torch.bfloat16, len(lens) + 1)
+    wide = torch.full((len(lens), -(-most // 16)), -1, dtype=I32, device="cuda")
+    wide[:, : table.shape[1]] = table
+    q.zero_()
+    q[:, :, 0] = 1.0
+    held = table[0, : -(-lens[0] // 16)].long()
+    k[held, :, :, 0] = -math.inf
+    out, lse = P.paged_attention(q, P.Pages(k, v), wide, n, with_lse=True)
+    assert out[0].isnan().all() and torch.isfinite(out[1:]).all()
+    j = lens[0] // 2
+    k[held[j // 16], 0, j % 16, 0] = 2.0
+    out, lse = P.paged_attention(q, P.Pages(k, v), wide, n, with_lse=True)
+    assert torch.equal(out[0], v[held[j // 16], 0, j % 16].expand(4, -1)) and ((lse[0] - 0.25).abs() <= 2.0 ** -22).all()
