@@ -440,7 +440,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
             for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
             const float top = fmaxf(m_run[nt][e], t);
             m_ref[nt][e] = top == -INFINITY ? 0.f : top;
-            m_most[nt][e] = top + PA_RAISE;
+            m_most[nt][e] = __fadd_rd(top, PA_RAISE);   // (down: no weight exceeds 2^8, however coarse fp32 is at these scores)
             alpha[e] = exp2_fast(m_run[nt][e] - m_ref[nt][e]);
             m_run[nt][e] = top;
             l_run[nt][e] *= alpha[e];

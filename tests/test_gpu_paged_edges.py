@@ -93,3 +93,24 @@ def test_scores_that_are_all_minus_infinity_are_not_absent(path, lens, most):
     k[held[j // 16], 0, j % 16, 0] = 2.0
     out, lse = P.paged_attention(q, P.Pages(k, v), wide, n, with_lse=True)
     assert torch.equal(out[0], v[held[j // 16], 0, j % 16].expand(4, -1)) and ((lse[0] - 0.25).abs() <= 2.0 ** -22).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("size", [2.0 ** e for e in range(20, 30)])
+def test_scores_whose_steps_are_coarse(size, dtype):
+    """Scores (in units of log 2) at which fp32 has steps of 1/8 to 64: a later key above the running scale by a few of them."""
+    import paper_2410_01805_b200 as P
+    n, step, dt = 200, max(size * 2.0 ** -23, 0.5), TYPES[dtype][0]   # (not divided: a block has its keys in two steps)
+    k = torch.zeros(13, 1, 16, 64, dtype=dt, device="cuda")
+    v = torch.randn(13, 1, 16, 64, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(dt)
+    q = torch.zeros(1, 1, 64, dtype=dt, device="cuda")
+    q[..., 0], q[..., 1] = 2.0 ** 10, 1.0
+    table, lens = torch.arange(13, dtype=I32, device="cuda")[None], torch.tensor([n], dtype=I32, device="cuda")
+    scale = size / 2.0 ** 20 * math.log(2.0)
+    for base, up in ((b, u) for b in (0, 1) for u in (1, 2, 3)):
+        k[..., 0], k[..., 1] = 2.0 ** 10, base * step / (size / 2.0 ** 20)
+        k[12, 0, 7, 1] = (base + up) * step / (size / 2.0 ** 20)
+        out, lse = P.paged_attention(q, P.Pages(k, v), table, lens, scale=scale, with_lse=True)
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all(), (up, out)
+        assert (out.double().abs() <= v.double().abs().amax((0, 2)) * (1 + 2.0 ** -8)).all()
