@@ -8,7 +8,7 @@
 //  * A warp takes 16 keys of each step and has a ring of stages of its own, filled by its own copies: no barrier of the block
 //    stands in the loop.  Keys are the m side of m16n8k16 tiles and the heads of a group (eight; sixteen in two tiles) the n
 //    side: S^T = K Q^T, O^T = V^T P^T, with an 8 x 8 transpose of P in between.
-//  * The softmax keeps a running scale per head that is raised only when a score exceeds it by 2^8 (then the 16 keys' maximum
+//  * The softmax keeps a running scale per head that is raised only when a weight would exceed 2^8 or 2^15 (then the 16 keys' maximum
 //    is found and the sums are rescaled): most steps need one vote in place of the reductions.
 //  * The warps of a block meet at the end of a (request, KV head); where the line was cut inside one, the blocks leave partial
 //    results that a second kernel joins, in the order of the blocks.
@@ -31,7 +31,13 @@ template <> struct PaCfg<128, 1> { static constexpr int WARPS = 5, STAGES = 2, P
 template <> struct PaCfg<96, 1> { static constexpr int WARPS = 5, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
 template <> struct PaCfg<64, 1> { static constexpr int WARPS = 7, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
 constexpr int PA_WHOLE = 6;        // steps up to which items are not divided (see launch)
-constexpr float PA_RAISE = 8.0f;   // log2 of how far a score may exceed the running scale
+// Log2 of a weight when the running scale is set, of the largest key so far, and of what one may reach until the scale is raised.
+// The second product takes a weight as the sum of two 16-bit numbers.  bf16 has the range for any of them, and 16 bits of each
+// (2^-17, against 2^-9 for the output's rounding) cost two products; more would cost three.  fp16 has 22 bits (2^-23) of a weight
+// from 2^-2 on, and of a smaller one what lies above 2^-25: so its weights lie as high as they can, and what is lost of a key is
+// at most 2^-36 of the largest key's weight (2^-25 with the bounds of bf16; 2^-32 and 2^-38, with 7 and 13, take the same time).
+template <typename T> struct PaWeight { static constexpr float SET = 0.f, MOST = 8.f; };
+template <> struct PaWeight<__half> { static constexpr float SET = 11.f, MOST = 15.f; };
 
 template <typename T>
 __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
@@ -357,6 +363,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   uint32_t qf[NT][KD][2], qn[NT][KD][2];
   bool first_item = true;
   int set = 0;
+  using Weight = PaWeight<T>;
   float o[NT][KD][4], m_run[NT][2], l_run[NT][2];
   float m_ref[NT][2], m_most[NT][2];   // the scale as it is subtracted (0 for -inf), and what a score may not exceed
   uint32_t seen = 0;                   // keys of the item that exist, over its steps
@@ -438,9 +445,10 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
             float t = fmaxf(s[nt][e], s[nt][e + 2]);
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
-            const float top = fmaxf(m_run[nt][e], t);
+            // (rounded so that no weight exceeds 2^MOST, however coarse fp32 is at these scores)
+            const float top = fmaxf(m_run[nt][e], Weight::SET == 0.f ? t : __fadd_ru(t, -Weight::SET));
             m_ref[nt][e] = top == -INFINITY ? 0.f : top;
-            m_most[nt][e] = __fadd_rd(top, PA_RAISE);   // (down: no weight exceeds 2^8, however coarse fp32 is at these scores)
+            m_most[nt][e] = __fadd_rd(top, Weight::MOST);
             alpha[e] = exp2_fast(m_run[nt][e] - m_ref[nt][e]);
             m_run[nt][e] = top;
             l_run[nt][e] *= alpha[e];

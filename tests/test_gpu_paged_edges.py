@@ -10,6 +10,8 @@ import paged_util as U
 from test_gpu_norm_rope import close, expected, f64, tensors, turns_of
 from test_gpu_paged_attention import I32, TYPES, check, make
 
+FP16_PEAK = 2.0 ** 11   # the least that the largest of a warp's weights in fp16 is
+
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,h,hk,d,rot", [(9, 5, 1, 128, 128), (33, 15, 5, 96, 96), (50, 3, 2, 64, 32), (7, 7, 3, 40, 16),
@@ -114,3 +116,31 @@ def test_scores_whose_steps_are_coarse(size, dtype):
         out, lse = P.paged_attention(q, P.Pages(k, v), table, lens, scale=scale, with_lse=True)
         assert torch.isfinite(out).all() and torch.isfinite(lse).all(), (up, out)
         assert (out.double().abs() <= v.double().abs().amax((0, 2)) * (1 + 2.0 ** -8)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("h,hk,d", [(8, 8, 64), (16, 4, 128), (32, 2, 96)])
+@pytest.mark.parametrize("n,nats", [(6500, 14.0), (6500, 17.0), (6500, 18.0), (30000, 17.0)])
+def test_many_weights_far_below_one(n, nats, h, hk, d, dtype):
+    """A first token far above all others whose value is zero: the output is that of the others, each weighing e^-nats."""
+    import paper_2410_01805_b200 as P
+    requests, page, dt = 64, 100, TYPES[dtype][0]   # (so many that a warp has thousands of the keys; all name the same pages)
+    pages = -(-n // page)
+    k = torch.zeros(pages, hk, page, d, dtype=dt, device="cuda")
+    v = torch.full_like(k, 64.0)
+    k[0, :, 0, 0], v[0, :, 0] = nats, 0.0
+    q = torch.zeros(requests, h, d, dtype=dt, device="cuda")
+    q[:, :, 0] = 1.0
+    table = torch.arange(pages, dtype=I32, device="cuda").repeat(requests, 1)
+    lens = torch.full((requests,), n, dtype=I32, device="cuda")
+    out, lse = P.paged_attention(q, P.Pages(k, v), table, lens, scale=1.0, with_lse=True)
+    tail = (n - 1) * math.exp(-nats)
+    want = 64 * tail / (1 + tail)
+    # The one rounding of the output; exp2, its argument (25 log2 units, 2^-19 of one) and the sums, which are equal terms:
+    # (n / 32 + 64) additions of 2^-23 (truncating ones allowed for); and of each fp16 weight what lies below 2^-25 when the largest is FP16_PEAK or more.
+    lost = (n - 1) * 2.0 ** -25 / FP16_PEAK * 64 if dtype == "fp16" else want * 2.0 ** -17
+    bound = TYPES[dtype][1] * want + 2.0 ** -25 + want * (2.0 ** -18 + (n / 32 + 64) * 2.0 ** -23) + lost
+    assert (out.double() - want).abs().max() <= bound
+    # (the sum, a one and n - 1 terms that may each be less than its step: no thread adds more than n / 32 + 64 of them)
+    assert (lse.double() - (nats + math.log1p(tail))).abs().max() <= 2.0 ** -20 * nats + (n / 32 + 64) * 2.0 ** -24
