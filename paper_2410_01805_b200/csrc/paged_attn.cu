@@ -309,9 +309,10 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   int row_page = 0, row_j = 0, row_key = 0;
   bool row_there = false;
   auto look_up = [&]() {
-    const int i = (solo ? load.tile : load.tile * PA_WARPS + warp) * 16 + (lane & 15);
-    row_there = i < load.v.n;
-    row_key = row_there ? load.v.key(i) : 0;
+    // (unsigned: of a request of nearly 2^31 tokens the last step ends behind them)
+    const uint32_t i = (uint32_t)(solo ? load.tile : load.tile * PA_WARPS + warp) * 16u + (lane & 15);
+    row_there = i < (uint32_t)load.v.n;
+    row_key = row_there ? load.v.key((int)i) : 0;
     row_j = a.by_size.div(row_key);
     row_page = row_there ? __ldg(load.row + row_j) : 0;
   };

@@ -144,3 +144,31 @@ def test_many_weights_far_below_one(n, nats, h, hk, d, dtype):
     assert (out.double() - want).abs().max() <= bound
     # (the sum, a one and n - 1 terms that may each be less than its step: no thread adds more than n / 32 + 64 of them)
     assert (lse.double() - (nats + math.log1p(tail))).abs().max() <= 2.0 ** -20 * nats + (n / 32 + 64) * 2.0 ** -24
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("h,hk,d", [(1, 1, 64), (2, 1, 128), (9, 1, 96)])
+def test_the_longest_request(h, hk, d):
+    """2^31 - 1 tokens, all in one page that its table names over and over: the last step of the line ends behind 2^31.  What
+    comes behind the request's row of the table is another request's page, whose values would show."""
+    import paper_2410_01805_b200 as P
+    page, width = 2 ** 15, 2 ** 16
+    k = torch.zeros(2, hk, page, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.ones_like(k)
+    v[1] = 2.0 ** 100
+    q = torch.zeros(2, h, d, dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros(2, width, dtype=I32, device="cuda")
+    table[1] = 1
+    lens, status = torch.tensor([2 ** 31 - 1, 5], dtype=I32, device="cuda"), torch.zeros(1, dtype=I32, device="cuda")
+    out, lse = P.paged_attention(q, P.Pages(k, v), table, lens, with_lse=True, status=status)
+    # scores of 0 and values of 1: sums of ones, equal to each other in every order, so their quotient is 1
+    assert status.item() == 0 and (out[0] == 1).all() and (out[1] == 2.0 ** 100).all()
+    # a sum of fewer than 2^24 ones is exact; 296 blocks of at most seven warps have no more of them each, and few sums of those
+    # are added: 2^-20 of the sum
+    assert (lse[0].double() - math.log(2 ** 31 - 1)).abs().max() <= 2.0 ** -19
+    # with a window: the newest two tokens and the first three
+    lens[1] = 2 ** 31 - 1
+    v[0, :, page - 3] = 2.0 ** 90   # (the next to newest: token 2^31 - 3)
+    v[0, :, 0] = 0.0
+    out = P.paged_attention(q, P.Pages(k, v), table, lens, window=2, sinks=3)
+    assert ((out[0].double() - 2.0 ** 90 / 5).abs() <= 2.0 ** 90 / 5 * 2.0 ** -8).all() and (out[1] == 2.0 ** 100).all()
