@@ -729,8 +729,9 @@ extern "C" int locret_paged_attention(const void *q, int64_t q_req, int64_t q_he
                                       int64_t out_req, int64_t out_head, float *lse, int32_t *status, void *workspace,
                                       int64_t workspace_bytes, void *stream) {
   if (!pages || !pages_ok(*pages) || !heads_ok(n_q_heads, pages->n_kv_heads, pages->head_dim)) return LOCRET_ERR_INVALID;
+  const float scale_log2 = scale * 1.4426950408889634f;   // (infinite, it would make NaN of a score of 0)
   if (n_req < 0 || n_req > LOCRET_MAX_REQUESTS || width < 1 || table_stride < 0 || (n_req > 1 && table_stride < width) ||
-      window < 0 || sinks < 0 || !isfinite(scale))
+      window < 0 || sinks < 0 || !isfinite(scale_log2))
     return LOCRET_ERR_INVALID;
   if ((q_req | q_head | out_req | out_head) & 7 || !aligned16p(q) || !aligned16p(out) || !aligned16p(workspace)) return LOCRET_ERR_INVALID;
   const long double span = (long double)(pages->n_pages - 1) * pages->page_stride + (long double)(pages->page_size - 1) * pages->token_stride +
@@ -757,7 +758,7 @@ extern "C" int locret_paged_attention(const void *q, int64_t q_req, int64_t q_he
   a.q_req = q_req; a.q_head = q_head; a.out_req = out_req; a.out_head = out_head;
   a.width = width; a.n_req = n_req; a.h = n_q_heads; a.h_kv = pages->n_kv_heads; a.groups = (g + hb - 1) / hb;
   a.window = window; a.sinks = sinks;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale_log2;
   long long most_keys = (long long)width * pages->page_size;
   if (window > 0 && (long long)window + sinks < most_keys) most_keys = (long long)window + sinks;
   const cudaError_t e = pages->dtype == LOCRET_BF16 ? launch_by_size<bf16>(a, pages->head_dim, hb / 8, most_keys, (cudaStream_t)stream)

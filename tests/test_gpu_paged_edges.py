@@ -172,3 +172,17 @@ def test_the_longest_request(h, hk, d):
     v[0, :, 0] = 0.0
     out = P.paged_attention(q, P.Pages(k, v), table, lens, window=2, sinks=3)
     assert ((out[0].double() - 2.0 ** 90 / 5).abs() <= 2.0 ** 90 / 5 * 2.0 ** -8).all() and (out[1] == 2.0 ** 100).all()
+
+
+def test_scales_that_fp32_cannot_hold_are_refused():
+    """Scores are kept in units of log 2: a scale is refused if its product with log2(e) is not finite in fp32."""
+    import ctypes as C
+    from paper_2410_01805_b200.binding import lib, locret_pages
+    pool = locret_pages(k=16, v=16, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, dtype=0, page_stride=2048, head_stride=1024,
+                        token_stride=64)
+    need = C.c_int64()
+    assert lib.locret_paged_attention_workspace(8, 2, 64, C.byref(need)) == 0
+    for scale, code in ((3e38, -1), (-3e38, -1), (2.4e38, -1), (2.3e38, 0), (-2.3e38, 0)):   # (FLT_MAX ln 2 = 2.3586e38)
+        # (no requests: the arguments are checked and nothing is launched)
+        assert lib.locret_paged_attention(None, 512, 64, C.byref(pool), None, 4, 4, None, 0, 8, scale, 0, 0, None, 512, 64, None, None,
+                                          None, need.value, None) == code, scale
