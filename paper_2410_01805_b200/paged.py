@@ -58,7 +58,7 @@ def rope_turns(rot: int, theta: float, scaling: dict | None = None, device="cuda
         def pair(turns):   # the pair (a real number) that makes this many turns within the original context
             return half * math.log(original / (turns * 2 * math.pi)) / math.log(theta)
         low = max(0.0, math.floor(pair(s.get("beta_fast", 32.0))))
-        high = min(half - 1.0, math.ceil(pair(s.get("beta_slow", 1.0))))
+        high = min(rot - 1.0, math.ceil(pair(s.get("beta_slow", 1.0))))   # (behind the last pair, if all turn that often)
         ramp = [min(1.0, max(0.0, (i - low) / max(high - low, 1e-3))) for i in range(half)]
         f = [x * ((1.0 - r) + r / s["factor"]) for x, r in zip(f, ramp)]
         factor = s.get("attention_factor", 0.1 * math.log(s["factor"]) + 1.0 if s["factor"] > 1 else 1.0)
