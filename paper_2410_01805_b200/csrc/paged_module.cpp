@@ -191,26 +191,34 @@ struct PagesObject {
 };
 extern PyTypeObject PagesType;
 
+locret_pages described(const at::Tensor &k, const at::Tensor &v) {
+  if (k.dim() != 4 || k.sizes() != v.sizes() || k.strides() != v.strides() || k.scalar_type() != v.scalar_type() || k.device() != v.device())
+    refuse("keys and values must be alike: [n_pages, n_kv_heads, page_size, head_dim]");
+  if (dtype_code(k.scalar_type()) < 0 || !k.is_cuda() || k.stride(3) != 1)
+    refuse("pages must be CUDA bfloat16 or float16 tensors, contiguous in the last dimension");
+  for (int i = 0; i < 4; i++)
+    if (k.size(i) > INT32_MAX) refuse("pages: a size does not fit 32 bits");
+  return {k.data_ptr(), v.data_ptr(), (int32_t)k.size(0), (int32_t)k.size(2), (int32_t)k.size(1), (int32_t)k.size(3),
+          dtype_code(k.scalar_type()), k.stride(0), k.stride(1), k.stride(2)};
+}
+// The struct as the tensors are now: a storage may have been replaced since the last call.
+const locret_pages &refreshed(PagesObject *p) {
+  return p->c = described(THPVariable_Unpack(p->k), THPVariable_Unpack(p->v));
+}
+
 PyObject *pages_new(PyTypeObject *type, PyObject *args, PyObject *kwargs) {
   return guarded([&]() -> PyObject * {
     static const char *names[] = {"k", "v", nullptr};
     PyObject *ko, *vo;
     if (!PyArg_ParseTupleAndKeywords(args, kwargs, "OO:Pages", const_cast<char **>(names), &ko, &vo)) throw Raised();
-    const at::Tensor &k = tensor(ko, "k"), &v = tensor(vo, "v");
-    if (k.dim() != 4 || k.sizes() != v.sizes() || k.strides() != v.strides() || k.scalar_type() != v.scalar_type() || k.device() != v.device())
-      refuse("keys and values must be alike: [n_pages, n_kv_heads, page_size, head_dim]");
-    if (dtype_code(k.scalar_type()) < 0 || !k.is_cuda() || k.stride(3) != 1)
-      refuse("pages must be CUDA bfloat16 or float16 tensors, contiguous in the last dimension");
-    for (int i = 0; i < 4; i++)
-      if (k.size(i) > INT32_MAX) refuse("pages: a size does not fit 32 bits");
+    const locret_pages c = described(tensor(ko, "k"), tensor(vo, "v"));
     PagesObject *self = reinterpret_cast<PagesObject *>(type->tp_alloc(type, 0));
     if (!self) throw Raised();
     Py_INCREF(ko);
     Py_INCREF(vo);
     self->k = ko;
     self->v = vo;
-    self->c = {k.data_ptr(), v.data_ptr(), (int32_t)k.size(0), (int32_t)k.size(2), (int32_t)k.size(1), (int32_t)k.size(3),
-               dtype_code(k.scalar_type()), k.stride(0), k.stride(1), k.stride(2)};
+    self->c = c;
     return reinterpret_cast<PyObject *>(self);
   });
 }
@@ -220,12 +228,16 @@ void pages_dealloc(PyObject *o) {
   Py_XDECREF(self->v);
   Py_TYPE(o)->tp_free(o);
 }
-PyObject *pages_address(PyObject *o, void *) { return PyLong_FromVoidPtr(&reinterpret_cast<PagesObject *>(o)->c); }
+PyObject *pages_address(PyObject *o, void *) {
+  return guarded([&]() -> PyObject * {
+    return PyLong_FromVoidPtr(const_cast<locret_pages *>(&refreshed(reinterpret_cast<PagesObject *>(o))));
+  });
+}
 
 PyMemberDef pages_members[] = {{"k", T_OBJECT_EX, offsetof(PagesObject, k), READONLY, "the keys' tensor"},
                                {"v", T_OBJECT_EX, offsetof(PagesObject, v), READONLY, "the values' tensor"},
                                {nullptr, 0, 0, 0, nullptr}};
-PyGetSetDef pages_getset[] = {{"address", pages_address, nullptr, "address of the C struct locret_pages, for the C entry points", nullptr},
+PyGetSetDef pages_getset[] = {{"address", pages_address, nullptr, "address of the C struct locret_pages as the tensors are now, for the C entry points", nullptr},
                               {nullptr, nullptr, nullptr, nullptr, nullptr}};
 PyTypeObject PagesType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
@@ -234,9 +246,9 @@ const locret_pages &pages_of(PyObject *o, const Where &w) {
     PyErr_SetString(PyExc_TypeError, "pages must be a Pages");
     throw Raised();
   }
-  const PagesObject *p = reinterpret_cast<PagesObject *>(o);
+  PagesObject *p = reinterpret_cast<PagesObject *>(o);
   if (THPVariable_Unpack(p->k).device() != w.device) refuse("pages must lie on " + w.device.str());
-  return p->c;
+  return refreshed(p);
 }
 
 // ---------------------------------------------------------------- pages_step

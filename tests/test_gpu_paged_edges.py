@@ -186,3 +186,26 @@ def test_scales_that_fp32_cannot_hold_are_refused():
         # (no requests: the arguments are checked and nothing is launched)
         assert lib.locret_paged_attention(None, 512, 64, C.byref(pool), None, 4, 4, None, 0, 8, scale, 0, 0, None, 512, 64, None, None,
                                           None, need.value, None) == code, scale
+
+
+@pytest.mark.gpu
+def test_pages_are_those_that_the_tensors_have_now():
+    """A pool whose storage was replaced under the same tensors: calls see the new one, or refuse what no longer fits."""
+    import paper_2410_01805_b200 as P
+    q, k, v, table, lens = make([40, 100], 4, 2, 64, 16, torch.bfloat16, 61)
+    old, new = torch.stack([k, v]), torch.stack([v, k]).contiguous()   # (the old storage stays)
+    k, v = old[0], old[1]
+    pages = P.Pages(k, v)
+    want = P.paged_attention(q, P.Pages(new[0], new[1]), table, lens)
+    k.data, v.data = new[0], new[1]
+    assert torch.equal(P.paged_attention(q, pages, table, lens), want)
+    x = torch.randn(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+    slots, pos = torch.tensor([3, 20], device="cuda"), torch.zeros(2, dtype=I32, device="cuda")
+    before = old.clone()
+    P.norm_rope(q, x, pos, P.rope_turns(64, 1e4)[0], v=x, pages=pages, slots=slots)
+    assert torch.equal(old.nan_to_num(), before.nan_to_num()) and torch.equal(new[:, 0, :, 3], x[:1].expand(2, -1, -1))
+    v.data = new[1, :-1]
+    for call in (lambda: P.paged_attention(q, pages, table, lens), lambda: pages.address,
+                 lambda: P.norm_rope(q, x, pos, P.rope_turns(64, 1e4)[0], v=x, pages=pages, slots=slots)):
+        with pytest.raises(ValueError):
+            call()
