@@ -3,13 +3,14 @@
 // small batch take, so these calls are checked, allocated for and launched here (4 to 9 us, one or two launches among them).
 //
 // Everything is as in the C entry points (include/locret.h), on torch's current stream; what can be seen of the tensors is checked
-// and refused with ValueError, what the library returns is raised as LocretError.
+// and refused with ValueError, what the library returns is raised as LocretError.  Autograd records none of the calls.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <structmember.h>
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -146,6 +147,12 @@ int32_t *status_word(PyObject *o, const Where &w) {
     refuse("status must be an int32 tensor on " + w.device.str());
   return static_cast<int32_t *>(t.data_ptr());
 }
+// The calls record nothing for autograd: an input that requires gradients would give outputs that silently have none.
+void no_graph(const at::Tensor &t, const char *what) {
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    refuse(std::string(what) + " requires gradients, which this call does not record: call it under torch.no_grad() or in the forward "
+                               "of a torch.autograd.Function (gradients of norm_rope: norm_rope_grad)");
+}
 // [tokens or requests, heads, d] of any strides whose last dimension is contiguous
 const at::Tensor &heads(PyObject *o, const char *what, at::ScalarType type, const Where &w) {
   const at::Tensor &t = tensor(o, what);
@@ -159,6 +166,7 @@ const at::Tensor &written(PyObject *o, const char *what, at::ScalarType type, co
   const at::Tensor &t = heads(o, what, type, w);
   for (int i = 0; i < 2; i++)
     if (t.size(i) > 1 && t.stride(i) == 0) refuse(std::string(what) + " is an expanded tensor");
+  no_graph(t, what);
   return t;
 }
 void same_shape(const at::Tensor &a, const at::Tensor &b, const char *what) {
@@ -247,7 +255,10 @@ const locret_pages &pages_of(PyObject *o, const Where &w) {
     throw Raised();
   }
   PagesObject *p = reinterpret_cast<PagesObject *>(o);
-  if (THPVariable_Unpack(p->k).device() != w.device) refuse("pages must lie on " + w.device.str());
+  const at::Tensor &k = THPVariable_Unpack(p->k), &v = THPVariable_Unpack(p->v);
+  if (k.device() != w.device) refuse("pages must lie on " + w.device.str());
+  no_graph(k, "the pages' k");
+  no_graph(v, "the pages' v");
   return refreshed(p);
 }
 
@@ -343,6 +354,8 @@ PyObject *norm_rope(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *k
     const Where w(q0, "q");
     const at::ScalarType type = q0.scalar_type();
     const at::Tensor &q = heads(a.v[0], "q", type, w), &k = heads(a.v[1], "k", type, w);
+    no_graph(q, "q");
+    no_graph(k, "k");
     if (k.size(0) != q.size(0) || k.size(2) != q.size(2)) refuse("q and k must have the same tokens and head size");
     if (!a.v[12] != !a.v[11] || !a.v[12] != !a.v[13]) refuse("pages, v and slots come together");
     locret_rope_args r = {};
@@ -354,11 +367,14 @@ PyObject *norm_rope(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *k
     if (a.v[12]) {
       const at::Tensor &v = heads(a.v[11], "v", type, w), *slots;
       same_shape(v, k, "v and k");
+      no_graph(v, "v");
       input(r.v, r.v_token, r.v_head, v);
       r.pages = &pages_of(a.v[12], w);
       r.slots = static_cast<int64_t *>(words(a.v[13], "slots", at::kLong, 1, w, &slots));
       if (slots->numel() != q.size(0)) refuse("one slot for every token");
     }
+    if (a.v[6]) no_graph(tensor(a.v[6], "g_q"), "g_q");
+    if (a.v[7]) no_graph(tensor(a.v[7], "g_k"), "g_k");
     rope_common(r, q, k.size(1), a.v[2], a.v[3], a.v[4], a.v[5], a.v[6], a.v[7], a.v[8], w);
     r.status = status_word(a.v[14], w);
     if (!a.v[9]) q_out = empty(q.sizes(), type, w);
@@ -433,6 +449,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObj
     const Where w(q0, "q");
     const locret_pages &pages = pages_of(a.v[1], w);
     const at::Tensor &q = heads(a.v[0], "q", q0.scalar_type(), w), *table, *lens;
+    no_graph(q, "q");
     if (dtype_code(q.scalar_type()) != pages.dtype || q.size(2) != pages.head_dim) refuse("q must have the pages' type and head size");
     void *const table_p = words(a.v[2], "table", at::kInt, 2, w, &table), *const lens_p = words(a.v[3], "lens", at::kInt, 1, w, &lens);
     if (table->size(0) != q.size(0) || lens->numel() != q.size(0)) refuse("one row of the table and one length for every request");
@@ -477,7 +494,8 @@ PyMethodDef methods[] = {
            "Per-head RMS norm (with gains g_q, g_k, if given), rotation at `positions` (int32 [n_tok]) and, with pages, the rotated\n"
            "keys and the values v into `slots` (int64 [n_tok], negative: none): q [n_tok, h, d], k and v [n_tok, h_kv, d], bf16 or\n"
            "fp16, of any token and head strides -> (q_out, k_out).  Outputs are allocated where none are given, k_out only without\n"
-           "pages; q_out may be q and k_out k.  turns, factor: of rope_turns."),
+           "pages; q_out may be q and k_out k.  turns, factor: of rope_turns.  Not recorded for autograd: inputs that require gradients\n"
+           "are refused unless recording is off, as in the forward of a torch.autograd.Function (norm_rope_grad in its backward)."),
     METHOD(norm_rope_grad,
            "norm_rope_grad(dq_out, dk_out, q, k, positions, turns, factor=1.0, interleaved=False, g_q=None, g_k=None, eps=1e-6)\n--\n\n"
            "Gradients of norm_rope from those of its outputs: (dq, dk, dg_q, dg_k), the latter fp32 [d] where a gain is given and\n"
@@ -486,7 +504,8 @@ PyMethodDef methods[] = {
            "paged_attention(q, pages, table, lens, scale=None, window=0, sinks=0, out=None, with_lse=False, status=None)\n--\n\n"
            "Attention of each request's newest token, q [n_req, h, d], over the keys and values in its pages: table int32\n"
            "[n_req, width], lens int32 [n_req] (the new token counted).  window > 0: only the last `window` and the first `sinks`\n"
-           "tokens are visible.  scale: 1 / sqrt(d) by default.  Returns out, [n_req, h, d], or (out, lse fp32 [n_req, h])."),
+           "tokens are visible.  scale: 1 / sqrt(d) by default.  Returns out, [n_req, h, d], or (out, lse fp32 [n_req, h]).  There is no\n"
+           "backward pass: inputs that require gradients are refused unless recording is off."),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", "Python entry points of the calls on pages.", -1, methods, nullptr, nullptr, nullptr, nullptr};

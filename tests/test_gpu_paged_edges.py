@@ -209,3 +209,55 @@ def test_pages_are_those_that_the_tensors_have_now():
                  lambda: P.norm_rope(q, x, pos, P.rope_turns(64, 1e4)[0], v=x, pages=pages, slots=slots)):
         with pytest.raises(ValueError):
             call()
+
+
+def _rotation_case():
+    import paper_2410_01805_b200 as P
+    q, k, v, (gq, gk), pos = tensors(4, 4, 2, 64, torch.bfloat16, 71, fused=False)
+    pool = torch.zeros(2, 3, 2, 16, 64, dtype=torch.bfloat16, device="cuda")
+    return P, q, k, v, gq, gk, pos, turns_of(64)[0], pool
+
+
+@pytest.mark.gpu
+def test_what_requires_gradients_is_not_dropped_silently():
+    P, q, k, v, gq, gk, pos, turns, pool = _rotation_case()
+    slots, pages = torch.arange(4, device="cuda"), P.Pages(pool[0], pool[1])
+    good = dict(q=q, k=k, positions=pos, turns=turns, g_q=gq, g_k=gk, v=v, pages=pages, slots=slots, q_out=torch.empty_like(q))
+    want, _ = P.norm_rope(**good)
+    want = want.clone()
+
+    def asks(t):
+        return t.detach().clone().requires_grad_(True)
+    bad = [{name: asks(good[name])} for name in ("q", "k", "v", "g_q", "g_k", "q_out")]
+    bad += [dict(pages=P.Pages(asks(pool[0]), asks(pool[1]))), dict(k_out=asks(k))]
+    for b in bad:
+        with pytest.raises(ValueError, match="requires gradients"):
+            P.norm_rope(**{**good, **b})
+        with torch.no_grad():
+            assert torch.equal(P.norm_rope(**{**good, **b})[0], want)
+    table, lens = torch.zeros(4, 1, dtype=I32, device="cuda"), torch.tensor([4, 3, 2, 1], dtype=I32, device="cuda")
+    attn = dict(q=q, pages=pages, table=table, lens=lens)
+    ref = P.paged_attention(**attn)
+    for b in (dict(q=asks(q)), dict(pages=P.Pages(asks(pool[0]), asks(pool[1]))), dict(out=asks(q))):
+        with pytest.raises(ValueError, match="requires gradients"):
+            P.paged_attention(**{**attn, **b})
+        with torch.no_grad():
+            assert torch.equal(P.paged_attention(**{**attn, **b}), ref)
+    # an operation of its own for autograd, as a model has it: forward and backward run with recording off
+    class Rotated(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, g_q, g_k):
+            ctx.save_for_backward(q, k, g_q, g_k)
+            return P.norm_rope(q, k, pos, turns, g_q=g_q, g_k=g_k)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            q, k, g_q, g_k = ctx.saved_tensors
+            d = P.norm_rope_grad(dq, dk, q, k, pos, turns, g_q=g_q, g_k=g_k)
+            return d[0], d[1], d[2].to(g_q.dtype), d[3].to(g_k.dtype)
+    leaves = [asks(t) for t in (q, k, gq, gk)]
+    a, b = Rotated.apply(*leaves)
+    dq, dk = torch.randn_like(a), torch.randn_like(b)
+    torch.autograd.backward([a, b], [dq, dk])
+    d = P.norm_rope_grad(dq, dk, q, k, pos, turns, g_q=gq, g_k=gk)
+    assert all(torch.equal(t.grad, x.to(t.dtype)) for t, x in zip(leaves, d))
