@@ -248,6 +248,9 @@ class LocretLayer:
             raise ValueError("pages, table_row and status (int32) must lie on the current device")
         _check(lib.locret_export_pages(self._h, pages.address, table_row.data_ptr(), table_row.numel(),
                                        status.data_ptr() if status is not None else None), "locret_export_pages")
+        for t in (pages.k, pages.v, status):   # (what autograd may have saved of them is no longer there)
+            if t is not None and not t.is_inference():
+                torch.autograd.graph.increment_version(t)
 
     def import_state_int4(self, Kc, Ks, Vc, Vs, S, T, seen: int):
         """Codes int8 [h_kv, len, d] in [-8, 7]; scales [h_kv, len] (values exact in fp16)."""

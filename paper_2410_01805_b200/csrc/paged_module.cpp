@@ -3,7 +3,8 @@
 // small batch take, so these calls are checked, allocated for and launched here (4 to 9 us, one or two launches among them).
 //
 // Everything is as in the C entry points (include/locret.h), on torch's current stream; what can be seen of the tensors is checked
-// and refused with ValueError, what the library returns is raised as LocretError.  Autograd records none of the calls.
+// and refused with ValueError, what the library returns is raised as LocretError.  Autograd records none of the calls; tensors that
+// they write in place count as changed.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <structmember.h>
@@ -153,6 +154,13 @@ void no_graph(const at::Tensor &t, const char *what) {
     refuse(std::string(what) + " requires gradients, which this call does not record: call it under torch.no_grad() or in the forward "
                                "of a torch.autograd.Function (gradients of norm_rope: norm_rope_grad)");
 }
+// What a call has written in place, for autograd's check that nothing saved for a backward pass has changed since.
+void changed(const at::Tensor &t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void changed(PyObject *o) {
+  if (o) changed(THPVariable_Unpack(o));
+}
 // [tokens or requests, heads, d] of any strides whose last dimension is contiguous
 const at::Tensor &heads(PyObject *o, const char *what, at::ScalarType type, const Where &w) {
   const at::Tensor &t = tensor(o, what);
@@ -249,6 +257,10 @@ PyGetSetDef pages_getset[] = {{"address", pages_address, nullptr, "address of th
                               {nullptr, nullptr, nullptr, nullptr, nullptr}};
 PyTypeObject PagesType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
+void changed_pages(PyObject *o) {
+  changed(reinterpret_cast<PagesObject *>(o)->k);
+  changed(reinterpret_cast<PagesObject *>(o)->v);
+}
 const locret_pages &pages_of(PyObject *o, const Where &w) {
   if (!PyObject_TypeCheck(o, &PagesType)) {
     PyErr_SetString(PyExc_TypeError, "pages must be a Pages");
@@ -301,6 +313,7 @@ PyObject *pages_step(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *
                             (int32_t)n_tok, static_cast<int64_t *>(slots.data_ptr()), static_cast<int32_t *>(positions.data_ptr()),
                             static_cast<int32_t *>(starts.data_ptr()), status_word(a.v[9], w), w.stream),
           "locret_pages_step");
+    for (PyObject *o : {a.v[0], a.v[3], lens_out, n_free_out, a.v[9]}) changed(o);
     PyObject *r = PyStructSequence_New(step_type);
     if (!r) throw Raised();
     Py_INCREF(lens_out);
@@ -386,6 +399,8 @@ PyObject *norm_rope(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObject *k
       output(r.k_out, r.k_out_token, r.k_out_head, k_out);
     }
     check(locret_norm_rope(&r, w.stream), "locret_norm_rope");
+    for (PyObject *o : {a.v[9], a.v[10], a.v[14]}) changed(o);
+    if (a.v[12]) changed_pages(a.v[12]);
     PyObject *qo = wrap(std::move(q_out)), *ko = k_out.defined() ? wrap(std::move(k_out)) : Py_NewRef(Py_None);
     PyObject *res = PyTuple_Pack(2, qo, ko);
     Py_DECREF(qo);
@@ -473,6 +488,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *argv, Py_ssize_t n, PyObj
                                  lse.defined() ? static_cast<float *>(lse.data_ptr()) : nullptr, status_word(a.v[9], w),
                                  ws.data_ptr(), need, w.stream),
           "locret_paged_attention");
+    for (PyObject *o : {a.v[7], a.v[9]}) changed(o);
     if (!lse.defined()) return wrap(std::move(out));
     PyObject *o = wrap(std::move(out)), *l = wrap(std::move(lse)), *res = PyTuple_Pack(2, o, l);
     Py_DECREF(o);

@@ -261,3 +261,55 @@ def test_what_requires_gradients_is_not_dropped_silently():
     torch.autograd.backward([a, b], [dq, dk])
     d = P.norm_rope_grad(dq, dk, q, k, pos, turns, g_q=gq, g_k=gk)
     assert all(torch.equal(t.grad, x.to(t.dtype)) for t, x in zip(leaves, d))
+
+
+@pytest.mark.gpu
+def test_what_is_written_in_place_counts_as_changed():
+    P, q, k, v, gq, gk, pos, turns, pool = _rotation_case()
+    slots, pages, status = torch.arange(4, device="cuda"), P.Pages(pool[0], pool[1]), torch.zeros(1, dtype=I32, device="cuda")
+
+    def versions(written, read, call):
+        before = [t._version for t in written + read]
+        call()
+        after = [t._version for t in written + read]
+        assert all(y > x for x, y in zip(before, after[: len(written)])) and before[len(written):] == after[len(written):]
+    q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+    versions([q_out, k_out, pool, status], [q, k, v, gq, gk, pos, turns, slots],
+             lambda: P.norm_rope(q, k, pos, turns, g_q=gq, g_k=gk, v=v, pages=pages, slots=slots, q_out=q_out, k_out=k_out, status=status))
+    table, lens, new = torch.zeros(4, 2, dtype=I32, device="cuda"), torch.ones(4, dtype=I32, device="cuda"), torch.ones(4, dtype=I32, device="cuda")
+    free, n_free = torch.arange(3, dtype=I32, device="cuda"), torch.tensor([0], dtype=I32, device="cuda")
+    versions([table, lens, free, n_free, status], [new], lambda: P.pages_step(table, lens, new, free, n_free, 16, 4, status=status))
+    lens_out, n_out = torch.empty_like(lens), torch.empty_like(n_free)
+    versions([table, lens_out, free, n_out], [lens, new, n_free],
+             lambda: P.pages_step(table, lens, new, free, n_free, 16, 4, lens_out=lens_out, n_free_out=n_out))
+    out = torch.empty_like(q)
+    versions([out, status], [q, pool, table, lens], lambda: P.paged_attention(q, pages, table, lens, out=out, status=status))
+    # so a backward pass that needs what was overwritten says so
+    x = q.detach().clone().requires_grad_(True)
+    y = (x * x).sum()
+    with torch.no_grad():
+        P.norm_rope(x, k, pos, turns, q_out=x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    # tensors of inference mode have no versions
+    with torch.inference_mode():
+        a, b = torch.empty_like(q), torch.empty_like(k)
+        P.norm_rope(q, k, pos, turns, q_out=a, k_out=b)
+    P.norm_rope(q, k, pos, turns, q_out=a, k_out=b)
+    assert torch.equal(a, P.norm_rope(q, k, pos, turns)[0])
+
+
+@pytest.mark.gpu
+def test_exported_pages_count_as_changed():
+    import paper_2410_01805_b200 as P
+    import workloads as W
+    from parity_util import bf16_dev
+    w = W.get_workload("c1_small_gqa")
+    sh = w.shape
+    layer = P.LocretLayer(sh, *[bf16_dev(x) for x in W.layer_weights(sh, 0)], 256, 128, 16)
+    layer.prefill_chunk(bf16_dev(W.hidden_states(w, 0, 128)), torch.empty(128, sh.n_q_heads * sh.head_dim, dtype=torch.bfloat16, device="cuda"))
+    pool = torch.zeros(2, 8, sh.n_kv_heads, 16, sh.head_dim, dtype=torch.bfloat16, device="cuda")
+    before = pool._version
+    layer.export_pages(P.Pages(pool[0], pool[1]), torch.arange(8, dtype=I32, device="cuda"))
+    assert pool._version > before
+    layer.destroy()
