@@ -4,6 +4,7 @@ without ctypes, _paged.so."""
 from __future__ import annotations
 
 import glob
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
@@ -36,8 +37,16 @@ def needs_build() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def built_for() -> str:
+    """The torch and Python that the module is compiled against: part of its documentation string, so that another one is noticed."""
+    return f"torch {importlib.metadata.version('torch')}, {sysconfig.get_config_var('SOABI')}"
+
+
 def module_needs_build() -> bool:
-    return not os.path.exists(MODULE) or any(os.path.getmtime(p) > os.path.getmtime(MODULE) for p in (MODULE_SRC, HEADER))
+    if not os.path.exists(MODULE) or any(os.path.getmtime(p) > os.path.getmtime(MODULE) for p in (MODULE_SRC, HEADER)):
+        return True
+    with open(MODULE, "rb") as f:
+        return f"({built_for()})".encode() not in f.read()
 
 
 def module_command():
@@ -46,8 +55,8 @@ def module_command():
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
-    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *("-I" + p for p in include), MODULE_SRC,
-            "-o", MODULE, "-L" + HERE, "-l:liblocret.so", "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch",
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *("-I" + p for p in include),
+            f'-DBUILT_FOR="{built_for()}"', MODULE_SRC, "-o", MODULE, "-L" + HERE, "-l:liblocret.so", "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch",
             "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"]
 
 
@@ -55,7 +64,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if force or needs_build():
         build_library(force, verbose)
     if force or module_needs_build():
-        subprocess.check_call(module_command())
+        try:
+            subprocess.check_call(module_command())
+        except (OSError, subprocess.CalledProcessError) as e:
+            raise RuntimeError("the library is built, the module for the calls on pages is not: it needs g++ and the headers of Python "
+                               f"and torch ({e}).  All else of the package works without it.") from e
     return LIB
 
 

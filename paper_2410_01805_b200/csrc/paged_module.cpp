@@ -524,7 +524,7 @@ PyMethodDef methods[] = {
            "backward pass: inputs that require gradients are refused unless recording is off."),
     {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", "Python entry points of the calls on pages.", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", "Python entry points of the calls on pages (" BUILT_FOR ").", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -7,7 +7,11 @@ import math
 
 import torch
 
-from . import _paged
+try:
+    from . import _paged
+except ImportError as e:
+    raise ImportError(f"the calls on pages need the compiled module _paged.so, which is missing or was built for another torch or "
+                      f"Python ({e}): run `python paper_2410_01805_b200/build.py`") from e
 from ._paged import Pages, PagesStep, norm_rope, norm_rope_grad, paged_attention, pages_step  # noqa: F401
 from .binding import LocretError
 
