@@ -439,6 +439,9 @@ int locret_adamw_step(float *param, void *param_bf16, const float *grad, float *
  * tokens' queries and keys, the latter with their values into the pages) and  locret_paged_attention.  A request that was
  * prefilled and evicted in a layer object enters the pool by  locret_export_pages.  Unit i of a request (i-th in temporal
  * order) sits at position i, as in a layer's cache (Section 3.4).
+ * Exported keys are rotated as the layer does it - halves of all head_dim elements, base rope_theta, factor 1 - and not normed:
+ * what  locret_norm_rope  adds to such a request has to be alike.  Scaled frequencies, interleaved pairs, a part of the head
+ * and norms are for requests all of whose keys it has written.
  *
  * None of these calls allocates, synchronises or keeps anything between calls: they may be captured into a graph, and calls on
  * several streams may overlap as long as they do not write the same memory (a workspace counts).  What the host cannot see -

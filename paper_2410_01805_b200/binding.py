@@ -240,7 +240,8 @@ class LocretLayer:
 
     def export_pages(self, pages, table_row: torch.Tensor, status: torch.Tensor | None = None):
         """The retained units into pages (a Pages): unit i into token i % page_size of page table_row[i // page_size].
-        Asynchronous on the layer's stream."""
+        Asynchronous on the layer's stream.  Their keys are rotated with rope_turns(head_dim, rope_theta) and not normed: norm_rope
+        has to rotate what it adds to them the same way, without gains."""
         if not (table_row.is_cuda and table_row.dtype == torch.int32 and table_row.dim() == 1 and table_row.is_contiguous()):
             raise ValueError("table_row must be a contiguous CUDA int32 vector")
         if pages.k.device != table_row.device or table_row.get_device() != torch.cuda.current_device() or (
