@@ -365,9 +365,10 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
   bool first_item = true;
   int set = 0;
   using Weight = PaWeight<T>;
-  float o[NT][KD][4], m_run[NT][2], l_run[NT][2];
-  float m_ref[NT][2], m_most[NT][2];   // the scale as it is subtracted (0 for -inf), and what a score may not exceed
-  uint32_t seen = 0;                   // keys of the item that exist, over its steps
+  // Sums, the scale (-inf: no key yet, and at the end of an item without one the output is 0), and what a score may not exceed: NaN
+  // before the first keys, which then set a scale whatever their scores are.  It is finite for keys whose scores are all -inf: their
+  // softmax is NaN, but beside others they weigh 0.
+  float o[NT][KD][4], m_run[NT][2], l_run[NT][2], m_most[NT][2];
   bool fresh = true;                   // the state belongs to no item yet
   int first_tile = 0, stage = 0;
   for (int left = n_steps; left > 0; left--) {
@@ -376,7 +377,6 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     const int4 step = info[warp][stage];
     if (fresh) {
       fresh = false;
-      seen = 0;
       first_tile = step.w;
       const int m = item_m(step.z), hg = item_hg(step.z);
       // the item's queries, requested when the last one began, and the next one's
@@ -396,8 +396,9 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
           for (int e = 0; e < 4; e++) o[nt][kk][e] = 0.f;
 #pragma unroll
         for (int e = 0; e < 2; e++) {
-          m_run[nt][e] = m_most[nt][e] = -INFINITY;
-          m_ref[nt][e] = l_run[nt][e] = 0.f;
+          m_run[nt][e] = -INFINITY;
+          m_most[nt][e] = NAN;
+          l_run[nt][e] = 0.f;
         }
       }
     }
@@ -410,7 +411,6 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
 
     const T *const ks = ring + stage * (S::STAGE / 2), *const vs = ks + 16 * LD;
     const uint32_t mask = step.x & 0xffff;
-    seen |= mask;
     if (mask) {
       float s[NT][4] = {};
 #pragma unroll
@@ -436,7 +436,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
 #pragma unroll
       for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) raise |= s[nt][e] > m_most[nt][e & 1];
+        for (int e = 0; e < 4; e++) raise |= !(s[nt][e] <= m_most[nt][e & 1]);
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
@@ -447,10 +447,9 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
             // (rounded so that no weight exceeds 2^MOST, however coarse fp32 is at these scores)
-            const float top = fmaxf(m_run[nt][e], Weight::SET == 0.f ? t : __fadd_ru(t, -Weight::SET));
-            m_ref[nt][e] = top == -INFINITY ? 0.f : top;
+            const float top = fmaxf(fmaxf(m_run[nt][e], -FLT_MAX), Weight::SET == 0.f ? t : __fadd_ru(t, -Weight::SET));
             m_most[nt][e] = __fadd_rd(top, Weight::MOST);
-            alpha[e] = exp2_fast(m_run[nt][e] - m_ref[nt][e]);
+            alpha[e] = exp2_fast(m_run[nt][e] - top);
             m_run[nt][e] = top;
             l_run[nt][e] *= alpha[e];
           }
@@ -469,7 +468,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
           float p[2];
 #pragma unroll
           for (int e = 0; e < 2; e++) {
-            p[e] = exp2_fast(s[nt][half * 2 + e] - m_ref[nt][e]);
+            p[e] = exp2_fast(s[nt][half * 2 + e] - m_run[nt][e]);
             l_run[nt][e] += p[e];
           }
           const uint32_t hi16 = Half2<T>::pack(p[0], p[1]);
@@ -491,14 +490,6 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
     __syncwarp();
 
     const bool ends = step.x >> 16 & 1;
-    // A scale of -inf says that there was no key (the output is 0).  Keys whose scores are all -inf, which give NaN, have the lowest
-    // finite one: beside others it makes a weight of 0 as well.
-    if (seen && (ends || left == 1)) {
-#pragma unroll
-      for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-        for (int e = 0; e < 2; e++) m_run[nt][e] = fmaxf(m_run[nt][e], -FLT_MAX);
-    }
     if (ends && solo) {
       // ---- the warp writes its item, half of the columns at a time through its own part of the buffer
       const int m = item_m(step.z), hg = item_hg(step.z), gh = min(HB, g - hg * HB);
