@@ -313,3 +313,35 @@ def test_exported_pages_count_as_changed():
     layer.export_pages(P.Pages(pool[0], pool[1]), torch.arange(8, dtype=I32, device="cuda"))
     assert pool._version > before
     layer.destroy()
+
+
+@pytest.mark.gpu
+def test_rotations_of_more_than_2_31_elements():
+    """4.6 GB of queries: the last tokens are what a call on them alone gives, forward and backward."""
+    import paper_2410_01805_b200 as P
+    n, h, hk, d, m = 560007, 32, 1, 128, 9
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.empty(n, h, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    k = torch.empty(n, hk, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    assert q.numel() > 2 ** 31
+    pos, turns = torch.arange(n, dtype=I32, device="cuda"), P.rope_turns(d, 1e4)[0]
+    gq = torch.empty(d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    out, k_out = P.norm_rope(q, k, pos, turns, g_q=gq)
+    want = P.norm_rope(q[-m:], k[-m:], pos[-m:], turns, g_q=gq)
+    assert torch.equal(out[-m:], want[0]) and torch.equal(k_out[-m:], want[1])
+    dq, dk, _, _ = P.norm_rope_grad(out, k_out, q, None, pos, turns, g_q=gq)
+    want = P.norm_rope_grad(out[-m:], k_out[-m:], q[-m:], None, pos[-m:], turns, g_q=gq)
+    assert torch.equal(dq[-m:], want[0]) and torch.equal(dk[-m:], want[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_positions_below_zero_turn_the_other_way(interleaved):
+    import paper_2410_01805_b200 as P
+    q, k, _, _, pos = tensors(40, 4, 2, 64, torch.bfloat16, 81, norm=False)
+    turns, _, freq = turns_of(64)
+    pos = -pos
+    pos[0] = -2 ** 31
+    got = P.norm_rope(q, k, pos, turns, interleaved=interleaved)
+    for x, y in zip((q, k), got):
+        close(y, *expected(x, None, 0.0, pos, freq, 1.0, interleaved), 2.0 ** -8)
