@@ -96,11 +96,8 @@ struct Ring {
   // a: the item's first run; ab: how far behind it the second lies
   template <typename T>
   __device__ __forceinline__ void request(int stage, int n, const T *a, int ab, bool ok, const T *safe) {
-    copy_item(stage, n, ok ? a : safe, ab, ok ? (int)sizeof(V) : 0);
-  }
-  template <typename T>   // bytes 0: nothing is read, the place is filled with zeros
-  __device__ __forceinline__ void copy_item(int stage, int n, const T *from, int ab, int bytes) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, bytes = ok ? (int)sizeof(V) : 0;   // (0: nothing is read, the place is filled with zeros)
+    const T *from = ok ? a : safe;
     copy(&v[stage][n][0][lane], from, bytes);
     copy(&v[stage][n][1][lane], from + ab, bytes);
   }
@@ -398,15 +395,11 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
     ask_x = src + tok * src_token + (long long)ask_head * src_head + it.a;
   };
   ask_from();
-  // A row that is not there has dy = 0, and x of the first row there is: with zeros and no epsilon the norm's factor would be infinite,
-  // and NaN reach the gains' sums.  (The first row is in these sums itself: what of it is not finite is there already.)
-  const T *const x_safe = it.there ? src + it.a : src;
-  const int x_bytes = it.there ? (int)sizeof(Raw<E>) / 2 : 0;
   auto ask = [&]() {
     if (ask_left > 0) {
       const bool ok = ask_head < rows && it.there;
       ring.request(fill, 0, ask_dy, ab, ok, dy);
-      if (g) ring.copy_item(fill, 1, ok ? ask_x : x_safe, ab, x_bytes);
+      if (g) ring.request(fill, 1, ask_x, ab, ok, src);
       ask_dy += dy_by;
       ask_x += x_by;
       ask_head += R;
@@ -434,6 +427,9 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
     const Turn<E> turn = turn_of<E, I, true>(pairs[warp], it, j, ones<E>());
     int head = s0 * R + row;
     T *to = dx + (tok * rows + head) * p.d + it.a;
+    // In a token's last step some rows may not be there, and are zeros: without an epsilon their factor would be infinite, and NaN reach
+    // the gains' sums.
+    const float last_eps = (s1 - 1) * R + row < rows ? p.eps : 1.f;
     for (int i = s1 - s0; i > 0; i--) {
       cp_async_wait<NRG_STAGES - 2>();
       P2<E> y = unpack2<T>(ring.get(stage, 0));
@@ -447,7 +443,7 @@ norm_rope_grad_kernel(const __grid_constant__ NormRope p, const __grid_constant_
 #pragma unroll
         for (int e = 0; e < E / 2; e++) w.v[e] = mul_f32x2(y.v[e], gain.v[e]);
         const float ss = group_sum<G>(dot2(x, x)), dot = group_sum<G>(dot2(w, x));
-        const float rstd = rsqrtf(fmaf(ss, p.inv_d, p.eps)), mean = dot * rstd * p.inv_d;
+        const float rstd = rsqrtf(fmaf(ss, p.inv_d, i == 1 ? last_eps : p.eps)), mean = dot * rstd * p.inv_d;
         const uint64_t r2 = both(rstd), m2 = both(-mean * rstd);
 #pragma unroll
         for (int e = 0; e < E / 2; e++) {
