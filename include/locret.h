@@ -547,12 +547,15 @@ int locret_norm_rope_grad(const locret_rope_args *args, void *d_q, void *d_k, fl
  * A request of length 0 gets zeros.  Pages that hold no visible key are not read, and their table entries not looked at.
  * Several requests may name the same pages.
  * q, out: type of the pool, element (r, j, c) at r * *_req + j * *_head + c, 16-byte aligned, strides multiples of 8; out
- * overlaps nothing that is read.  lse: fp32 [n_req x h] or NULL, the logarithm of the sum of exp(scale * q . k) (-inf for length 0).  table, lens: device int32 as in
- * locret_pages_step; a length outside [0, width * page_size] is taken as the nearer end, a key in a page that does not exist
- * as absent, both reported.  scale: any number whose product with log2(e) is finite in fp32 (1 / sqrt(d) in Eq. 1).  head_dim 64, 96 or 128; h a multiple of h_kv;
+ * overlaps nothing that is read.  lse: fp32 [n_req x h] or NULL, the logarithm of the sum of exp(scale * q . k) (-inf without a
+ * key).  table, lens: device int32 as in locret_pages_step; a length outside [0, width * page_size] is taken as the nearer end, a
+ * key in a page that does not exist as absent (a request without any other gets zeros), both reported.  scale: any number whose
+ * product with log2(e) is finite in fp32 (1 / sqrt(d) in Eq. 1).  head_dim 64, 96 or 128; h a multiple of h_kv;
  * 0 <= n_req <= LOCRET_MAX_REQUESTS.
  * Scores, softmax and sums in fp32; the probabilities enter the second product as the sum of two 16-bit numbers: off by at most
- * 2^-17 of each (bf16), 2^-23 of each or 2^-36 of the largest that its warp has seen (fp16).
+ * 2^-17 of each (bf16), 2^-23 of each or 2^-36 of the largest that its warp has seen (fp16).  Scores that are all -inf give NaN,
+ * as in softmax.  A visible value that is not finite makes NaN, or that infinity, of its column in every head that sees it; what
+ * is not visible is not read.
  * workspace: device memory, 16-byte aligned, at least the bytes that locret_paged_attention_workspace reports for the current
  * device; contents need not be kept, and two calls that may overlap need one each.
  */

@@ -6,8 +6,8 @@
 
 namespace locret {
 
-// n / d for 0 <= n < 2^31: n * ceil(2^(31 + s) / d) >> (31 + s) with s = ceil(log2 d), exact because the factor is too large by
-// less than 2^s / d * 2^-(31 + s) of itself.
+// n / d for 0 <= n < 2^31: n * ceil(2^(31 + s) / d) >> (31 + s) with s = ceil(log2 d).  Exact: the factor exceeds 2^(31 + s) / d by
+// less than 1, so the quotient by less than n * 2^-(31 + s) < 2^-s <= 1 / d, which does not reach the next whole number.
 struct FastDiv {
   uint32_t mul, shift;
   FastDiv() = default;

@@ -33,7 +33,7 @@ template <> struct PaCfg<64, 1> { static constexpr int WARPS = 7, STAGES = 2, PE
 constexpr int PA_WHOLE = 6;        // steps up to which items are not divided (see launch)
 // Log2 of a weight when the running scale is set, of the largest key so far, and of what one may reach until the scale is raised.
 // The second product takes a weight as the sum of two 16-bit numbers.  bf16 has the range for any of them, and 16 bits of each
-// (2^-17, against 2^-9 for the output's rounding) cost two products; more would cost three.  fp16 has 22 bits (2^-23) of a weight
+// (2^-17, against 2^-8 for the output's rounding) cost two products; more would cost three.  fp16 has 22 bits (2^-23) of a weight
 // from 2^-2 on, and of a smaller one what lies above 2^-25: so its weights lie as high as they can, and what is lost of a key is
 // at most 2^-36 of the largest key's weight (2^-25 with the bounds of bf16; 2^-32 and 2^-38, with 7 and 13, take the same time).
 template <typename T> struct PaWeight { static constexpr float SET = 0.f, MOST = 8.f; };
