@@ -31,13 +31,14 @@ template <> struct PaCfg<128, 1> { static constexpr int WARPS = 5, STAGES = 2, P
 template <> struct PaCfg<96, 1> { static constexpr int WARPS = 5, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
 template <> struct PaCfg<64, 1> { static constexpr int WARPS = 7, STAGES = 2, PER_SM = 2; static constexpr bool TWO = true; };
 constexpr int PA_WHOLE = 6;        // steps up to which items are not divided (see launch)
-// Log2 of a weight when the running scale is set, of the largest key so far, and of what one may reach until the scale is raised.
-// The second product takes a weight as the sum of two 16-bit numbers.  bf16 has the range for any of them, and 16 bits of each
-// (2^-17, against 2^-8 for the output's rounding) cost two products; more would cost three.  fp16 has 22 bits (2^-23) of a weight
-// from 2^-2 on, and of a smaller one what lies above 2^-25: so its weights lie as high as they can, and what is lost of a key is
-// at most 2^-36 of the largest key's weight (2^-25 with the bounds of bf16; 2^-32 and 2^-38, with 7 and 13, take the same time).
-template <typename T> struct PaWeight { static constexpr float SET = 0.f, MOST = 8.f; };
-template <> struct PaWeight<__half> { static constexpr float SET = 11.f, MOST = 15.f; };
+// A key's weight is 1 where it sets the running scale, and at most 2^MOST before the scale is raised.  The second product takes it,
+// times UP, as the sum of two 16-bit numbers.  bf16 has the range for any of them, and 16 bits of each (2^-17, against 2^-8 for the
+// output's rounding) cost two products; more would cost three.  fp16 has 22 bits (2^-23) of a number from 2^-2 on, and of a smaller one
+// what lies above 2^-25: so its weights are carried as high as they can be, and what is lost of a key is at most 2^-36 of the largest
+// key's weight (2^-25 with UP 1 and MOST 8; the same time: 24 requests, a window of 4096, 32 heads of 96, 177 us).  The sums of
+// weights go without UP: as 11 in the exponent it cost no product, but each weight, and the logarithm of the sum, 2^-21.
+template <typename T> struct PaWeight { static constexpr float MOST = 8.f, UP = 1.f; };
+template <> struct PaWeight<__half> { static constexpr float MOST = 4.f, UP = 2048.f; };
 
 template <typename T>
 __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
@@ -446,9 +447,8 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
             float t = fmaxf(s[nt][e], s[nt][e + 2]);
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
-            // (rounded so that no weight exceeds 2^MOST, however coarse fp32 is at these scores)
-            const float top = fmaxf(fmaxf(m_run[nt][e], -FLT_MAX), Weight::SET == 0.f ? t : __fadd_ru(t, -Weight::SET));
-            m_most[nt][e] = __fadd_rd(top, Weight::MOST);
+            const float top = fmaxf(fmaxf(m_run[nt][e], -FLT_MAX), t);
+            m_most[nt][e] = __fadd_rd(top, Weight::MOST);   // (down: no weight exceeds 2^MOST, however coarse fp32 is at these scores)
             alpha[e] = exp2_fast(m_run[nt][e] - top);
             m_run[nt][e] = top;
             l_run[nt][e] *= alpha[e];
@@ -470,6 +470,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
           for (int e = 0; e < 2; e++) {
             p[e] = exp2_fast(s[nt][half * 2 + e] - m_run[nt][e]);
             l_run[nt][e] += p[e];
+            p[e] *= Weight::UP;
           }
           const uint32_t hi16 = Half2<T>::pack(p[0], p[1]);
           const float2 back = Half2<T>::unpack(hi16);
@@ -516,7 +517,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
           for (int x = lane; x < 8 * (D / 8); x += 32) {
             const int hh = x / (D / 8), c = (x - hh * (D / 8)) * 4, head = nt * 8 + hh, col = side * (D / 2) + c;
             if (head >= gh) continue;
-            const float top = wm[0][warp][head], l = wl[0][warp][head], inv = top == -INFINITY ? 0.f : 1.0f / l;
+            const float top = wm[0][warp][head], l = wl[0][warp][head], inv = top == -INFINITY ? 0.f : 1.0f / (l * PaWeight<T>::UP);
             const float4 f = *reinterpret_cast<const float4 *>(mine + hh * LF + c);
             const int j = m * g + hg * HB + head;
             *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + step.y * a.out_req + j * a.out_head + col) =
@@ -570,7 +571,7 @@ paged_attn_kernel(const __grid_constant__ PagedAttn a) {
             }
             const int j = m * g + hg * HB + head;
             if (whole) {
-              const float inv = top == -INFINITY ? 0.f : 1.0f / l;
+              const float inv = top == -INFINITY ? 0.f : 1.0f / (l * PaWeight<T>::UP);
               *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + step.y * a.out_req + j * a.out_head + col) =
                   make_uint2(Half2<T>::pack(sum.x * inv, sum.y * inv), Half2<T>::pack(sum.z * inv, sum.w * inv));
               if (a.lse && col == 0) a.lse[(size_t)step.y * a.h + j] = top == -INFINITY ? top : (top + log2f(l)) * 0.6931471805599453f;
@@ -664,7 +665,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) paged_join_kernel(const __gri
     l += ls[s];
   }
   const int j = m * g + hg * HB + head;
-  const float inv = top == -INFINITY ? 0.f : 1.0f / l;   // (no part has seen a key)
+  const float inv = top == -INFINITY ? 0.f : 1.0f / (l * PaWeight<T>::UP);   // (no part has seen a key)
   *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + r * a.out_req + j * a.out_head + lane * 4) =
       make_uint2(Half2<T>::pack(acc.x * inv, acc.y * inv), Half2<T>::pack(acc.z * inv, acc.w * inv));
   if (a.lse && lane == 0) a.lse[(size_t)r * a.h + j] = top == -INFINITY ? top : (top + log2f(l)) * 0.6931471805599453f;

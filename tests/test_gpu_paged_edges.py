@@ -345,3 +345,25 @@ def test_positions_below_zero_turn_the_other_way(interleaved):
     got = P.norm_rope(q, k, pos, turns, interleaved=interleaved)
     for x, y in zip((q, k), got):
         close(y, *expected(x, None, 0.0, pos, freq, 1.0, interleaved), 2.0 ** -8)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_the_logarithm_of_one_weight_is_its_score(dtype, d):
+    """Requests of one key and of four equal ones, scores from 2^-16 to 2^10, each a single exact product."""
+    import paper_2410_01805_b200 as P
+    dt, scores = TYPES[dtype][0], torch.tensor([s * 2.0 ** e for e in range(-16, 11) for s in (1.0, -1.25)], dtype=torch.float64)
+    n = len(scores)
+    k = torch.zeros(n, 1, 4, d, dtype=dt, device="cuda")
+    k[:, :, :, 3] = scores.to(dt).cuda()[:, None, None]
+    q = torch.zeros(n, 1, d, dtype=dt, device="cuda")
+    q[..., 3] = 1.0
+    table = torch.arange(n, dtype=I32, device="cuda")[:, None]
+    for keys in (1, 4):
+        _, lse = P.paged_attention(q, P.Pages(k, torch.ones_like(k)), table, torch.full((n,), keys, dtype=I32, device="cuda"), scale=1.0,
+                                   with_lse=True)
+        want = scores + math.log(keys)
+        # log2(e), the score in units of log 2, the sum, ln 2 and the last product: five roundings of 2^-24 (the logarithm of 4 is exact)
+        bound = 5 * 2.0 ** -24 * (scores.abs() + math.log(keys))
+        assert ((lse[:, 0].double().cpu() - want).abs() <= bound).all()
