@@ -8,7 +8,7 @@
 //  * A warp takes 16 keys of each step and has a ring of stages of its own, filled by its own copies: no barrier of the block
 //    stands in the loop.  Keys are the m side of m16n8k16 tiles and the heads of a group (eight; sixteen in two tiles) the n
 //    side: S^T = K Q^T, O^T = V^T P^T, with an 8 x 8 transpose of P in between.
-//  * The softmax keeps a running scale per head that is raised only when a weight would exceed 2^8 or 2^15 (then the 16 keys' maximum
+//  * The softmax keeps a running scale per head that is raised only when a weight would exceed 2^8, fp16 2^4 (then the 16 keys' maximum
 //    is found and the sums are rescaled): most steps need one vote in place of the reductions.
 //  * The warps of a block meet at the end of a (request, KV head); where the line was cut inside one, the blocks leave partial
 //    results that a second kernel joins, in the order of the blocks.
